@@ -363,7 +363,8 @@ def _prepare_own(st, case):
         st["y"], st["dx"], st["dw"] = like(m, n, kind), like(m, k, kind), like(n, k, torch.float32)
     else:
         rows, top = case["rows"], case["top"]
-        st["logprob"], st["entropy"], st["lse"] = (torch.empty(rows, device="cuda") for _ in range(3))
+        st["logprob"], st["entropy"] = (torch.empty(rows, device="cuda") for _ in range(2))
+        st["lse"] = like(rows, 2, torch.float32)
         st["top_logprob"] = like(rows, top, torch.float32) if top else None
         st["top_ids"] = like(rows, top, torch.int64) if top else None
         if case["grad"]:
