@@ -323,6 +323,84 @@ int excp_set_param(excp_ctx *ctx, int param, uint64_t value);
  * counters with. */
 int excp_copy_probe(excp_ctx *ctx, void *dst, const void *src, uint64_t nbytes);
 
+/* ---- Operators on reconstructed weights: 4-bit microscaled products and token log probabilities ----
+ *
+ * What a reconstructed checkpoint is answered and trained with.  The calls below are enqueued on the
+ * context's stream and return; they report argument errors at once and have no data-dependent ones, so
+ * nothing is collected, and they may be called while a batch is pending.  They allocate nothing.  All
+ * pointers are device memory; a matrix is row-major, its element (i, j) at i * ld + j, ld >= columns;
+ * inputs and outputs do not overlap unless a call says so.  Sizes are below 2^31, offsets are 64 bits.
+ * Arrays are aligned to their element; code arrays to 16 B and scale arrays to 4 B. */
+#define EXCP_TYPE_F32   0            /* element types of the matrices */
+#define EXCP_TYPE_F16   1
+#define EXCP_TYPE_BF16  2
+#define EXCP_MAX_DIM    2147483647ull
+
+/* Microscaled 4-bit floating point ("MX", E2M1 elements under E8M0 scales, blocks of 32 along a row).
+ *   scale of a block: 2^e, e = floor(log2(largest |x|)) - 2, not below -127; stored as the byte e + 127.
+ *   element: x / 2^e to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0..7), ties to the even code,
+ *            beyond 6 to 6; bit 3 is the sign.
+ *   A block of zeros has byte 0; a block that holds a NaN or an infinity has byte 255 and stands for NaN.
+ * A row of `cols` elements takes ceil(cols / 128) groups: 64 B of codes a group, two to a byte, the even
+ * element in the low half, and 4 B of scales.  What a group holds beyond `cols` is written as zeros by
+ * excp_mx_quantize and has to be zero codes where a product reads it. */
+uint64_t excp_mx_code_bytes(uint64_t rows, uint64_t cols);    /* rows * 64 * ceil(cols / 128) */
+uint64_t excp_mx_scale_bytes(uint64_t rows, uint64_t cols);   /* rows *  4 * ceil(cols / 128) */
+
+/* x (rows x cols) -> codes and scales of its rows, and (or) codes_t and scales_t of its columns, i.e. of
+ * x transposed (cols x rows).  Either pair may be NULL, not both.  One read of x serves both. */
+int excp_mx_quantize(excp_ctx *ctx, const void *x, int type, uint64_t rows, uint64_t cols, uint64_t ld,
+                     void *codes, void *scales, void *codes_t, void *scales_t);
+/* The values that codes and scales stand for, rounded once to `type` (fp32 and, but for values below its
+ * normal range, bf16 hold them exactly). */
+int excp_mx_dequantize(excp_ctx *ctx, const void *codes, const void *scales, uint64_t rows, uint64_t cols,
+                       void *x, int type, uint64_t ld);
+
+/* y (m x n) = A B^T, A (m x k) and B (n x k) in codes and scales: sums of products in fp32, rounded once
+ * to `type`.  With A = x and B = W it is a layer's output; with dy, W^T its input's gradient; with dy^T,
+ * x^T its weights' -- the transposed operands are what excp_mx_quantize writes to codes_t. */
+int excp_mx_matmul(excp_ctx *ctx, const void *a_codes, const void *a_scales, const void *b_codes,
+                   const void *b_scales, uint64_t m, uint64_t n, uint64_t k, void *y, int type, uint64_t ld);
+
+/* y (m x n) = MX(x) W^T for x in 16 or 32 bits: excp_mx_quantize of x and excp_mx_matmul in one call, with
+ * the same result.  x_codes and x_scales (sizes as above for m x k) are room to work in; what they hold
+ * afterwards is unspecified.  They may be NULL for up to EXCP_MX_FEW_ROWS rows, which need none. */
+#define EXCP_MX_FEW_ROWS 16
+int excp_mx_linear(excp_ctx *ctx, const void *x, int x_type, uint64_t ldx, const void *w_codes,
+                   const void *w_scales, uint64_t m, uint64_t n, uint64_t k, void *y, int y_type, uint64_t ldy,
+                   void *x_codes, void *x_scales);
+
+/* For every row of logits (rows x vocab): lse = log sum_i exp(x_i), logprob = x[target] - lse, entropy =
+ * -sum_i p_i log p_i with p_i = exp(x_i - lse), and the `ntop` largest x_i - lse with their indices, in
+ * descending order, equal logits by ascending index.  All statistics in fp32; one read of the logits.
+ *   A logit of -inf is a masked token: p = 0, never an alternative; as a target its logprob is -inf.
+ *   A target outside [0, vocab) is none: logprob 0.
+ *   Alternatives that do not exist (fewer than ntop unmasked tokens) have index -1 and logprob -inf.
+ *   A row with nothing unmasked: lse -inf, entropy 0, no alternatives.
+ *   A row that holds a NaN or +inf: NaN statistics and log probabilities; its alternatives' indices
+ *   are the order of its other tokens (+inf first, NaN never).
+ * lse is written in two parts (rows x 2), the largest unmasked logit and the log of the sum of exp(x_i -
+ * largest): their sum would lose the second one beside logits of a large magnitude (a mask's lowest
+ * value in all of a row).  A row with nothing unmasked: -inf and 0.
+ * logprob, entropy (rows each), lse, top_logprob and top_ids (rows x ntop) may each be NULL, targets
+ * too if logprob is; ntop <= EXCP_MAX_TOP. */
+#define EXCP_MAX_TOP 64
+int excp_token_logprobs(excp_ctx *ctx, const void *logits, int type, uint64_t rows, uint64_t vocab, uint64_t ld,
+                        const int64_t *targets, int ntop, float *logprob, float *entropy, float *lse,
+                        float *top_logprob, int64_t *top_ids);
+
+/* The gradient over the logits of sum_r g_logprob[r] logprob[r] + g_entropy[r] entropy[r]
+ * + sum_j g_top[r][j] top_logprob[r][j]:
+ *   d_i = g_logprob ([i = target] - p_i) + sum_j g_top_j ([i = top_ids_j] - p_i) - g_entropy p_i (log p_i + entropy)
+ * from the lse and entropy (needed with g_entropy) that excp_token_logprobs wrote.  Each g may be NULL (zero); targets are
+ * needed with g_logprob, top_ids with g_top.  What has no value in a row -- no target, a masked target,
+ * index -1 -- takes no part, and a row with nothing unmasked gets zeros.  dlogits has the logits' type and
+ * its own ld, and may be the logits' own array (ldd = ld then). */
+int excp_token_logprobs_backward(excp_ctx *ctx, const void *logits, int type, uint64_t rows, uint64_t vocab,
+                                 uint64_t ld, const int64_t *targets, const float *lse, const float *entropy,
+                                 const int64_t *top_ids, int ntop, const float *g_logprob, const float *g_entropy,
+                                 const float *g_top, void *dlogits, uint64_t ldd);
+
 /* Bytes of device workspace the context holds. */
 uint64_t excp_workspace_bytes(const excp_ctx *ctx);
 

@@ -18,7 +18,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libexcp.so")
 LIB_SAN = os.path.join(HERE, "libexcp_hostsan.so")
-SOURCES = ["excp_host.hip", "k_stats.hip", "k_mask.hip", "k_kmeans.hip", "k_small.hip", "k_decode.hip"]
+SOURCES = ["excp_host.hip", "k_stats.hip", "k_mask.hip", "k_kmeans.hip", "k_small.hip", "k_decode.hip",
+           "op_host.hip", "k_mx_quant.hip", "k_mx_product.hip", "k_logprobs.hip"]
 FLAGS = [
     "-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-shared",
     "-ffp-contract=off",                       # every fp operation rounds once, as the method is defined

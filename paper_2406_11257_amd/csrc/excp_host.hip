@@ -12,6 +12,7 @@
 
 #include "../../include/excp.h"
 #include "excp_device.h"
+#include "excp_ops.h"
 
 namespace {
 
@@ -52,6 +53,8 @@ struct excp_ctx {
     // descriptors and tile tables of a call, one after the other (see Staged): pinned, and the device's copy
     unsigned char *h_stage = nullptr, *d_stage = nullptr;
     HostRec *h_rec = nullptr;
+    struct RowPart *row_parts = nullptr;     // of the operators on rows of logits (see excp_ops.h)
+    u32 *row_tickets = nullptr;
     u64 ws_bytes = 0;
     std::vector<void *> allocs;
     // pending batch
@@ -285,6 +288,8 @@ int static_device(int device, StaticDevice &out) {
 }
 
 }  // namespace
+
+OpsContext excp_ops_context(const excp_ctx *c) { return {c->device, c->stream, (u32)c->w.cus, c->row_parts, c->row_tickets, c->broken}; }
 
 extern "C" {
 
