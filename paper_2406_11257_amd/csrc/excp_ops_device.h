@@ -32,6 +32,15 @@ __device__ __forceinline__ Eight<T> load_some(const T *p, u32 have) {
     return r;
 }
 
+// Four consecutive elements in one write, where rows begin at multiples of four.
+template <class T>
+__device__ __forceinline__ bool store4_aligned(const T *p, u64 ld) { return (((u64)p | ld * sizeof(T)) & (4u * sizeof(T) - 1u)) == 0u; }
+template <class T>
+__device__ __forceinline__ void store4(T *p, v4f32 v) {
+    struct alignas(4 * sizeof(T)) { T e[4]; } q = {{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}};
+    __builtin_memcpy(__builtin_assume_aligned(p, 4 * sizeof(T)), &q, sizeof q);
+}
+
 // Scale byte of a block from the largest of its magnitudes' bits: floor(log2) - 2 of a normal number is its exponent
 // field less 2 (biased alike), of a smaller one below the least there is; 255 for a NaN or an infinity.
 __device__ __forceinline__ u32 mx_scale_byte(u32 peak_bits) {
@@ -62,10 +71,22 @@ __device__ __forceinline__ void mx_values(u32 codes, float *q) {
 }
 
 // acc += A B^T over 128 elements, for 16 rows of either; lane l holds the 32 codes of row l % 16 from element
-// 32 * (l / 16) on, and their scale in the low byte of its scale register.  Result: lane l holds rows
+// 32 * (l / 16) on, and their scale in byte BYTE of its scale register.  Result: lane l holds rows
 // 4 * (l / 16) .. + 3 of A against row l % 16 of B.
+template <int BYTE = 0>
 __device__ __forceinline__ v4f32 mx_mfma(v4i32 a, u32 sa, v4i32 b, u32 sb, v4f32 acc) {
     const v8i32 x = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
     const v8i32 y = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, 0, (int)sa, 0, (int)sb);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, BYTE, (int)sa, BYTE, (int)sb);
+}
+
+// Memory to LDS without registers: every lane's 16 (4) bytes from its own address, to `to` (the same in every lane)
+// plus 16 (4) times the lane's number.
+typedef const __attribute__((address_space(1))) void *global_bytes;
+typedef __attribute__((address_space(3))) void *lds_bytes;
+__device__ __forceinline__ void load16_to_lds(const unsigned char *from, unsigned char *to) {
+    __builtin_amdgcn_global_load_lds((global_bytes)from, (lds_bytes)to, 16, 0, 0);
+}
+__device__ __forceinline__ void load4_to_lds(const unsigned char *from, unsigned char *to) {
+    __builtin_amdgcn_global_load_lds((global_bytes)from, (lds_bytes)to, 4, 0, 0);
 }

@@ -149,6 +149,25 @@ def test_matmul(ctx, m, n, k, dtype):
     assert torch.equal(again, y)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(3500, 3700, 600), (4100, 3333, 1280), (2049, 8190, 384), (1500, 1700, 2944), (5000, 3900, 127), (50304, 300, 256)])
+def test_matmul_of_many_tiles(ctx, m, n, k, dtype):
+    """The same at sizes that fill the GPU with the larger tiles (compared in 64 bits on the GPU)."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m + n + k)
+    (ca, cb), values = (X.mx_empty(m, k), X.mx_empty(n, k)), []
+    for (codes, scales), rows, scale in ((ca, m, 1.0), (cb, n, 0.02)):
+        a = torch.empty(rows, k, device="cuda").normal_(0, scale, generator=g)
+        ctx.excp_mx_quantize(a, codes, scales)
+        ctx.excp_mx_dequantize(codes, scales, a)
+        values.append(a.double())
+    y = torch.empty(m, n, dtype=DTYPES[dtype], device="cuda")
+    ctx.excp_mx_matmul(*ca, *cb, k, y)
+    want, size = values[0] @ values[1].t(), values[0].abs() @ values[1].abs().t()
+    bound = (-(-k // 128) + 16) * 2.0 ** -22 * size + HALF_ULP[dtype] * size + SMALLEST[dtype]
+    assert bool(((y.double() - want).abs() <= bound).all())
+
+
 @pytest.mark.parametrize("xtype,ytype", [("f32", "f32"), ("f16", "f32"), ("bf16", "bf16"), ("bf16", "f16"), ("f32", "bf16"), ("f16", "f16")])
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
 def test_linear_quantises_on_the_way(ctx, m, n, k, xtype, ytype):
