@@ -358,7 +358,9 @@ int excp_mx_dequantize(excp_ctx *ctx, const void *codes, const void *scales, uin
 
 /* y (m x n) = A B^T, A (m x k) and B (n x k) in codes and scales: sums of products in fp32, rounded once
  * to `type`.  With A = x and B = W it is a layer's output; with dy, W^T its input's gradient; with dy^T,
- * x^T its weights' -- the transposed operands are what excp_mx_quantize writes to codes_t. */
+ * x^T its weights' -- the transposed operands are what excp_mx_quantize writes to codes_t.  k is at most
+ * EXCP_MX_MAX_K. */
+#define EXCP_MX_MAX_K 33554432ull
 int excp_mx_matmul(excp_ctx *ctx, const void *a_codes, const void *a_scales, const void *b_codes,
                    const void *b_scales, uint64_t m, uint64_t n, uint64_t k, void *y, int type, uint64_t ld);
 

@@ -16,52 +16,124 @@ __device__ __forceinline__ float widen(__bf16 x) { return (float)x; }
 // Eight consecutive elements, as they are stored: 16 B of a 16-bit type, 32 B of floats.
 template <class T> struct Eight { T v[8]; };
 
-// One read in 16-byte pieces (p is 16-byte aligned).
+// The first `have` of eight elements, zeros after them.  (Whole ones in pieces of 16 bytes, wherever they begin.)
 template <class T>
-__device__ __forceinline__ Eight<T> load_eight(const T *p) {
+__device__ __forceinline__ Eight<T> load_eight(const T *p, u32 have) {
     Eight<T> r;
-    __builtin_memcpy(&r, __builtin_assume_aligned(p, 16), sizeof r);
-    return r;
-}
-// `have` elements one by one (any alignment), zeros after them.
-template <class T>
-__device__ __forceinline__ Eight<T> load_some(const T *p, u32 have) {
-    Eight<T> r;
+    if (have >= 8u) {
+        __builtin_memcpy(&r, p, sizeof r);
+    } else {
 #pragma unroll
-    for (u32 i = 0; i < 8; ++i) r.v[i] = i < have ? p[i] : (T)0;
+        for (u32 i = 0; i < 8; ++i) r.v[i] = i < have ? p[i] : (T)0;
+    }
+    return r;
+}
+template <class T>
+__device__ __forceinline__ void store_eight(T *p, const Eight<T> &r, u32 have) {
+    if (have >= 8u) {
+        __builtin_memcpy(p, &r, sizeof r);
+    } else {
+#pragma unroll
+        for (u32 i = 0; i < 8; ++i)
+            if (i < have) p[i] = r.v[i];
+    }
+}
+template <class T>
+__device__ __forceinline__ u32 word_of(const Eight<T> &r, u32 i) {      // two elements of a 16-bit type
+    u32 w[4];
+    __builtin_memcpy(w, &r, sizeof w);
+    return w[i];
+}
+
+// Rows that can be written in pieces of 16 bytes.
+template <class T>
+__device__ __forceinline__ bool rows_aligned(const T *p, u64 ld) { return (((u64)p | ld * sizeof(T)) & 15u) == 0u; }
+// Elements at .. at + N - 1 of a row of `end`, as they are stored, in one write where the row allows it.
+template <class T, u32 N>
+__device__ __forceinline__ void store_run(T *row, u32 at, u32 end, bool there, bool wide, uint4 v) {
+    static_assert(N * sizeof(T) == 16, "");
+    if (there && wide && at + N <= end) {
+        *(uint4 *)(row + at) = v;
+    } else if (there) {
+        T e[N];
+        __builtin_memcpy(e, &v, 16);
+#pragma unroll
+        for (u32 i = 0; i < N; ++i)
+            if (at + i < end) row[at + i] = e[i];
+    }
+}
+// Four floats rounded to a 16-bit type.
+template <class T>
+__device__ __forceinline__ uint2 pack4(v4f32 v) {
+    const T e[4] = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+    uint2 r;
+    __builtin_memcpy(&r, e, 8);
     return r;
 }
 
-// Four consecutive elements in one write, where rows begin at multiples of four.
-template <class T>
-__device__ __forceinline__ bool store4_aligned(const T *p, u64 ld) { return (((u64)p | ld * sizeof(T)) & (4u * sizeof(T) - 1u)) == 0u; }
-template <class T>
-__device__ __forceinline__ void store4(T *p, v4f32 v) {
-    struct alignas(4 * sizeof(T)) { T e[4]; } q = {{(T)v[0], (T)v[1], (T)v[2], (T)v[3]}};
-    __builtin_memcpy(__builtin_assume_aligned(p, 4 * sizeof(T)), &q, sizeof q);
+// Quantisation of a block, in steps that lanes share: the largest magnitude (in the type's own bits, which order as the
+// magnitudes do, infinities and NaN above all), the scale byte from it, the codes.
+typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
+typedef __bf16 v2bf16 __attribute__((ext_vector_type(2)));
+typedef _Float16 v2f16 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32 max_halves(u32 a, u32 b) {               // of the two 16-bit halves, each
+    return __builtin_bit_cast(u32, __builtin_elementwise_max(__builtin_bit_cast(v2u16, a), __builtin_bit_cast(v2u16, b)));
 }
-
-// Scale byte of a block from the largest of its magnitudes' bits: floor(log2) - 2 of a normal number is its exponent
-// field less 2 (biased alike), of a smaller one below the least there is; 255 for a NaN or an infinity.
-__device__ __forceinline__ u32 mx_scale_byte(u32 peak_bits) {
-    const int e = (int)(peak_bits >> 23);
+__device__ __forceinline__ u32 mx_peak(const Eight<float> &x) {
+    u32 r = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r = max(r, f2u(x.v[i]) & 0x7fffffffu);
+    return r;
+}
+template <class T>
+__device__ __forceinline__ u32 mx_peak(const Eight<T> &x) {
+    u32 r = word_of(x, 0) & 0x7fff7fffu;
+#pragma unroll
+    for (u32 i = 1; i < 4; ++i) r = max_halves(r, word_of(x, i) & 0x7fff7fffu);
+    return max(r & 0xffffu, r >> 16);
+}
+// floor(log2) - 2 of a normal number is its exponent field less 2 (biased alike), of a smaller one below the least there
+// is; 255 for a NaN or an infinity.
+template <class T>
+__device__ __forceinline__ u32 mx_scale_byte(u32 peak) {
+    if constexpr (sizeof(T) == 2) peak = f2u(widen(__builtin_bit_cast(T, (unsigned short)peak)));
+    const int e = (int)(peak >> 23);
     return e == 255 ? 255u : (u32)max(e - 2, 0);
 }
-// 2^-(e) of a scale byte e + 127: a normal number for every byte that a finite block has (0 .. 252).
-__device__ __forceinline__ float mx_inverse(u32 byte) { return u2f((254u - byte) << 23); }
-// 2^e: below the normal range for byte 0, NaN for 255.
+// 2^e of a scale byte e + 127: below the normal range for byte 0, NaN for 255.
 __device__ __forceinline__ float mx_power(u32 byte) { return byte == 255u ? u2f(0x7fc00000u) : u2f(byte ? byte << 23 : 0x00400000u); }
-
-// Codes of eight elements already divided by their scale.  The conversion rounds to nearest even and saturates; the
-// division is a multiplication before it, which is exact wherever the quotient matters (a quotient below the normal
-// range rounds to zero either way).
-__device__ __forceinline__ u32 mx_codes(const float *q) {
+// 2^-e: a normal number for every byte that a finite block has (0 .. 252).
+__device__ __forceinline__ float mx_inverse(u32 byte) { return u2f((254u - byte) << 23); }
+// The codes of eight elements; of a block that holds an infinity or a NaN, zeros.  The conversions divide by a power of
+// two, round to the nearest of the grid, ties to the even code, and saturate.  (Floats are multiplied by the inverse first:
+// the instruction takes no scale below the normal range.)
+__device__ __forceinline__ u32 mx_codes(const Eight<float> &x, u32 byte) {
+    const float s = mx_inverse(byte);
     u32 r = 0;
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, q[0], q[1], 1.0f, 0);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, q[2], q[3], 1.0f, 1);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, q[4], q[5], 1.0f, 2);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, q[6], q[7], 1.0f, 3);
-    return r;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[0] * s, x.v[1] * s, 1.0f, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[2] * s, x.v[3] * s, 1.0f, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[4] * s, x.v[5] * s, 1.0f, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, x.v[6] * s, x.v[7] * s, 1.0f, 3);
+    return byte == 255u ? 0u : r;
+}
+__device__ __forceinline__ u32 mx_codes_of_words(u32 a, u32 b, u32 c, u32 d, float s, __bf16) {
+    u32 r = 0;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(v2bf16, a), s, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(v2bf16, b), s, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(v2bf16, c), s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(r, __builtin_bit_cast(v2bf16, d), s, 3);
+}
+__device__ __forceinline__ u32 mx_codes_of_words(u32 a, u32 b, u32 c, u32 d, float s, _Float16) {
+    u32 r = 0;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, __builtin_bit_cast(v2f16, a), s, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, __builtin_bit_cast(v2f16, b), s, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, __builtin_bit_cast(v2f16, c), s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(r, __builtin_bit_cast(v2f16, d), s, 3);
+}
+template <class T>
+__device__ __forceinline__ u32 mx_codes(const Eight<T> &x, u32 byte) {
+    const u32 r = mx_codes_of_words(word_of(x, 0), word_of(x, 1), word_of(x, 2), word_of(x, 3), mx_power(byte), T());
+    return byte == 255u ? 0u : r;
 }
 // and back
 __device__ __forceinline__ void mx_values(u32 codes, float *q) {

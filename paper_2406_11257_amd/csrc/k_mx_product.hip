@@ -12,8 +12,12 @@ struct Tile {
     static constexpr u32 codes = rows * 128u, stage = codes + rows * 8u;    // bytes: a row's codes, and its two groups' scales
     static constexpr u32 chunks = rows / 8u / waves;                        // loads a wave: 8 rows of codes each
     static constexpr u32 scale_loads = rows / 32u / waves;                  // and 32 rows of scales each
+    static constexpr int loads = chunks + scale_loads;
     static_assert(rows % (32u * waves) == 0, "");
     static constexpr int ahead = 2, before = 2 * TN - (TN + 1) / 2;         // steps (see the kernel)
+    // loads issued before step i of the after + before - gap steps over which they are spread
+    static constexpr int after = 2 * TN - before, spread = 2 * TN - (TN / 2 + 1);
+    static constexpr int loaded_by(int i) { return i >= spread ? loads : loads * i / spread; }
     // fragments read before step q begins
     static constexpr int read_by(int q) {
         const int for_step = q + ahead;
@@ -70,22 +74,23 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
         const u32 row = (wave * L::scale_loads + c) * 32u + (lane >> 1);
         scale_at[c] = (row < L::bn ? min(row, n_last) : min(row - L::bn, m_last)) * scale_pitch + (lane & 1u) * 4u;
     }
-    // groups `first` and `first` + 1 (of a lone group: twice the same)
-    auto fetch = [&](unsigned char *buf, u32 first, u32 back_codes, u32 back_scales) __attribute__((always_inline)) {
-#pragma unroll
-        for (u32 c = 0; c < L::chunks; ++c) {
-            const u32 chunk = wave * L::chunks + c;
-            u32 at = code_at[c] - back_codes;
+    // Groups `first` and `first` + 1 (of a lone group: twice the same): load `c` of what this wave brings in.
+    auto load = [&](unsigned char *buf, u32 first, u32 back_codes, u32 back_scales, auto index) __attribute__((always_inline)) {
+        constexpr u32 c = decltype(index)::value;
+        if constexpr (c >= L::scale_loads) {
+            const u32 chunk = wave * L::chunks + (c - L::scale_loads);
+            u32 at = code_at[c - L::scale_loads] - back_codes;
             asm volatile("" : "+v"(at));                     // (as in `hidden`: no pointer a load kept and moved on)
             load16_to_lds((chunk * 8u < L::bn ? b_codes : a_codes) + first * 64u + at, buf + chunk * 1024u);
-        }
-#pragma unroll
-        for (u32 c = 0; c < L::scale_loads; ++c) {
+        } else {
             const u32 chunk = wave * L::scale_loads + c;
             u32 at = scale_at[c] - back_scales;
             asm volatile("" : "+v"(at));
             load4_to_lds((chunk * 32u < L::bn ? b_scales : a_scales) + first * 4u + at, buf + L::codes + chunk * 256u);
         }
+    };
+    auto fetch = [&](unsigned char *buf, u32 first, u32 back_codes, u32 back_scales) __attribute__((always_inline)) {
+        static_for<0, L::loads>([&](auto c) __attribute__((always_inline)) { load(buf, first, back_codes, back_scales, c); });
     };
     const u32 rn = wn * TN * 16u + r, rm = L::bn + wm * TM * 16u + r;
     // Where this lane's parts of the fragments lie.
@@ -120,13 +125,12 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
         constexpr int s = decltype(index)::value / TN, i = decltype(index)::value % TN;
 #pragma unroll
         for (int j = 0; j < TM; ++j) acc[i][j] = mx_mfma(n_frag[s][i], n_scale[s][i], m_frag[s][j], m_scale[s][j], acc[i][j]);
-    };
-    // The products up to here are not put off until after what follows.
-    auto done = [&]() __attribute__((always_inline)) {
+        // (the products are not put off until after what follows)
 #pragma unroll
-        for (int i = 0; i < TN; ++i)
-#pragma unroll
-            for (int j = 0; j < TM; ++j) asm volatile("" : "+v"(acc[i][j]));
+        for (int j = 0; j < TM; ++j) {
+            if constexpr (L::waves > 4) asm volatile("" : "+v"(acc[i][j]));
+            else asm volatile("" : "+a"(acc[i][j]));
+        }
     };
     // All loads to LDS that this wave has issued are there; with the barrier after it, those of all waves.
     auto landed = []() __attribute__((always_inline)) {
@@ -137,21 +141,31 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
         const Places at = hidden();
         static_for<0, L::read_by(-1)>([&](auto f) __attribute__((always_inline)) { read(buf, at, f); });
     };
+    // Loads are spread over the steps: many in a row would keep a wave from its products until the last has been taken.
+    // Those of the next stage but one begin after the barrier that frees their buffer and end in the next stage.
     auto stage = [&](unsigned char *cur, unsigned char *next, u32 t) __attribute__((always_inline)) {
         const Places at = hidden();
         static_for<0, L::before>([&](auto q) __attribute__((always_inline)) {
+            if (t + 1u < stages)
+                static_for<L::loaded_by(L::after + q), L::loaded_by(L::after + q + 1)>([&](auto c) __attribute__((always_inline)) {
+                    load(next, lone + 2u * (t + 1u), 0u, 0u, c);
+                });
             static_for<L::read_by(q - 1), L::read_by(q)>([&](auto f) __attribute__((always_inline)) { read(cur, at, f); });
             __builtin_amdgcn_sched_barrier(0);
             step(q);
             __builtin_amdgcn_sched_barrier(0);
         });
-        done();
         landed();                                            // `next` is there, and `cur` has been read by all
-        if (t + 2u < stages) fetch(cur, lone + 2u * (t + 2u), 0u, 0u);
         begin(next);                                         // (after the last stage: whatever is there, and unused)
-        __builtin_amdgcn_sched_barrier(0);
-        static_for<L::before, 2 * TN>(step);
-        done();
+        static_for<L::before, 2 * TN>([&](auto q) __attribute__((always_inline)) {
+            if (t + 2u < stages)
+                static_for<L::loaded_by(q - L::before), L::loaded_by(q - L::before + 1)>([&](auto c) __attribute__((always_inline)) {
+                    load(cur, lone + 2u * (t + 2u), 0u, 0u, c);
+                });
+            __builtin_amdgcn_sched_barrier(0);
+            step(q);
+            __builtin_amdgcn_sched_barrier(0);
+        });
     };
     if (lone) {
         fetch(even, 0, (piece & 4u) * 16u, (lane & 1u) * 4u);
@@ -164,74 +178,116 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
     if (stages) {
         fetch(even, lone, 0u, 0u);
         landed();
-        if (1u < stages) fetch(odd, lone + 2u, 0u, 0u);
+        if (1u < stages)
+            static_for<0, L::loaded_by(L::after)>([&](auto c) __attribute__((always_inline)) { load(odd, lone + 2u, 0u, 0u, c); });
         begin(even);
         for (u32 t = 0; t < stages; t += 2u) {
             stage(even, odd, t);
             if (t + 1u < stages) stage(odd, even, t + 1u);
         }
     }
-    const bool wide = store4_aligned((const T *)p.y, p.ld);
+    // A lane holds four consecutive elements of a row of y, sixteen apart.  Of a 16-bit type that would be 32 bytes of a row
+    // a write: the lanes of two neighbouring fragments trade halves first, and it is 64.
+    const bool wide = rows_aligned((const T *)p.y, p.ld);
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
         const u32 m = m0 + (wm * TM + j) * 16u + r;
-        if (m >= p.m) continue;
-        T *y = (T *)p.y + (u64)m * p.ld;
+        T *y = (T *)p.y + (u64)min(m, p.m - 1u) * p.ld;
 #pragma unroll
-        for (int i = 0; i < TN; ++i) {
-            const u32 n = n0 + (wn * TN + i) * 16u + g * 4u;
-            if (wide && n + 4u <= p.n) {
-                store4(y + n, acc[i][j]);
+        for (int i = 0; i < TN; i += 2) {
+            const u32 n = n0 + (wn * TN + i) * 16u;
+            if constexpr (sizeof(T) == 2) {
+                const uint2 a = pack4<T>(acc[i][j]), b = pack4<T>(acc[i + 1][j]);
+                const auto lo = __builtin_amdgcn_permlane16_swap(a.x, b.x, false, false), hi = __builtin_amdgcn_permlane16_swap(a.y, b.y, false, false);
+                store_run<T, 8>(y, n + (g & 1u) * 16u + (g >> 1) * 8u, p.n, m < p.m, wide, make_uint4(lo[0], hi[0], lo[1], hi[1]));
             } else {
 #pragma unroll
-                for (u32 e = 0; e < 4; ++e)
-                    if (n + e < p.n) y[n + e] = (T)acc[i][j][e];
+                for (int k = 0; k < 2; ++k)
+                    store_run<T, 4>(y, n + k * 16u + g * 4u, p.n, m < p.m, wide, __builtin_bit_cast(uint4, acc[i + k][j]));
             }
         }
     }
 }
 
-// Up to sixteen rows of x, quantised on the way: a lane's 32 elements are a block.  Sixteen rows of W a workgroup;
-// its waves share the reduction and join their sums in LDS.
-template <class X, class T>
-__global__ __launch_bounds__(256) void k_mx_few_rows(const MxProduct p) {
-    __shared__ v4f32 part[4][64];
-    const u32 lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane & 15u, g = lane >> 4;
-    for (u32 n0 = blockIdx.x * 16u; n0 < p.n; n0 += gridDim.x * 16u) {
-    v4f32 acc = {};
-    for (u32 k = wave; k < p.groups; k += 4u) {
-        const u64 rw = (u64)min(n0 + r, p.n - 1u) * p.groups + k;
-        const v4i32 w = *(const v4i32 *)(p.b_codes + rw * 64u + g * 16u);
-        const u32 sw = p.b_scales[rw * 4u + g];
-        float v[32];
-        u32 peak = 0;
+// Few rows of A: the rows of B are read once, each by one wave, and that is the time it takes.  A workgroup has 16 TN rows
+// of B against 16 TM rows of A; its eight waves take the groups of the reduction in turn (so that together they read runs
+// of 512 bytes), straight into registers, and join their sums in LDS.  X: the type of A before its quantisation, where a
+// lane's 32 elements are a block that it quantises itself; void: codes.
+template <class X, class T, int TN, int TM>
+__global__ __launch_bounds__(512) void k_mx_few_rows(const MxProduct p) {
+    constexpr u32 kWaves = 8, kFragments = TN * TM;
+    __shared__ v4f32 part[kWaves][kFragments][64];
+    const u32 lane = lane_id(), wave = threadIdx.x >> 6, r = lane & 15u, g = lane >> 4;
+    const u32 tiles_n = (p.n + 16u * TN - 1u) / (16u * TN), tiles = tiles_n * ((p.m + 16u * TM - 1u) / (16u * TM));
+    for (u32 tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const u32 n0 = (tile % tiles_n) * 16u * TN, m0 = (tile / tiles_n) * 16u * TM;
+    const unsigned char *b_row[TN], *b_scale[TN];
 #pragma unroll
-        for (u32 i = 0; i < 32; ++i) {
-            const u32 j = k * 128u + g * 32u + i;
-            v[i] = r < p.m && j < p.x.cols ? widen(((const X *)p.x.p)[r * p.x.ld + j]) : 0.0f;
-            peak = max(peak, f2u(v[i]) & 0x7fffffffu);
+    for (int i = 0; i < TN; ++i) {
+        const u64 at = (u64)min(n0 + i * 16u + r, p.n - 1u) * p.groups;
+        b_row[i] = p.b_codes + at * 64u + g * 16u;
+        b_scale[i] = p.b_scales + at * 4u + g;
+    }
+    v4f32 acc[TN][TM] = {};
+    for (u32 k = wave; k < p.groups; k += kWaves) {
+        v4i32 n_frag[TN], m_frag[TM];
+        u32 n_scale[TN], m_scale[TM];
+#pragma unroll
+        for (int i = 0; i < TN; ++i) {
+            n_frag[i] = *(const v4i32 *)(b_row[i] + k * 64ull);
+            n_scale[i] = b_scale[i][k * 4ull];
         }
-        const u32 byte = mx_scale_byte(peak);
-        const float inv = byte == 255u ? 0.0f : mx_inverse(byte);
-        v4i32 x;
 #pragma unroll
-        for (u32 i = 0; i < 4; ++i) {
-            float q[8];
+        for (int j = 0; j < TM; ++j) {
+            const u32 m = m0 + j * 16u + r;
+            if constexpr (std::is_void<X>::value) {
+                const u64 at = (u64)min(m, p.m - 1u) * p.groups + k;
+                m_frag[j] = *(const v4i32 *)(p.a_codes + at * 64u + g * 16u);
+                m_scale[j] = p.a_scales[at * 4u + g];
+            } else {
+                const u32 col = k * 128u + g * 32u, have = m < p.m && col < p.x.cols ? p.x.cols - col : 0u;
+                const X *x = (const X *)p.x.p + (u64)m * p.x.ld + col;
+                Eight<X> e[4];
+                u32 peak = 0;
 #pragma unroll
-            for (u32 j = 0; j < 8; ++j) q[j] = byte == 255u ? 0.0f : v[i * 8 + j] * inv;
-            x[i] = (int)mx_codes(q);
+                for (u32 q = 0; q < 4; ++q) {
+                    e[q] = load_eight(x + q * 8u, have > q * 8u ? have - q * 8u : 0u);
+                    peak = max(peak, mx_peak(e[q]));
+                }
+                m_scale[j] = mx_scale_byte<X>(peak);
+#pragma unroll
+                for (u32 q = 0; q < 4; ++q) m_frag[j][q] = (int)mx_codes(e[q], m_scale[j]);
+            }
         }
-        acc = mx_mfma(w, sw, x, byte, acc);
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int j = 0; j < TM; ++j) acc[i][j] = mx_mfma(n_frag[i], n_scale[i], m_frag[j], m_scale[j], acc[i][j]);
+    }
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j) part[wave][i * TM + j][lane] = acc[i][j];
+    __syncthreads();
+    for (u32 f = wave; f < kFragments; f += kWaves) {
+        v4f32 sum = part[0][f][lane];
+#pragma unroll
+        for (u32 w = 1; w < kWaves; ++w) sum += part[w][f][lane];
+        const u32 n = n0 + (f / TM) * 16u + g * 4u, m = m0 + (f % TM) * 16u + r;
+        if (m >= p.m) continue;
+        T *y = (T *)p.y + (u64)m * p.ld + n;
+#pragma unroll
+        for (u32 e = 0; e < 4; ++e)
+            if (n + e < p.n) y[e] = (T)sum[e];
     }
     __syncthreads();
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (wave) continue;
-    acc = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-#pragma unroll
-    for (u32 e = 0; e < 4; ++e)
-        if (n0 + g * 4u + e < p.n && r < p.m) ((T *)p.y)[(u64)r * p.ld + n0 + g * 4u + e] = (T)acc[e];
     }
+}
+
+template <class X, class T, int TN, int TM>
+void launch_few(const MxProduct &p, hipStream_t s) {
+    const u32 tiles = ((p.n + 16u * TN - 1u) / (16u * TN)) * ((p.m + 16u * TM - 1u) / (16u * TM));
+    k_mx_few_rows<X, T, TN, TM><<<std::min(tiles, 1u << 20), 512, 0, s>>>(p);
 }
 
 }  // namespace
@@ -246,6 +302,12 @@ void launch_tiles(const MxProduct &p, hipStream_t s) {
 void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
     with_type(p.type, [&](auto tag) {
         using T = decltype(tag);
+        if (p.m <= 64u) {
+            if (p.m <= 16u) launch_few<void, T, 1, 1>(p, s);
+            else if (p.m <= 32u) launch_few<void, T, 2, 2>(p, s);
+            else launch_few<void, T, 1, 4>(p, s);
+            return;
+        }
         const u64 large = (u64)((p.n + 255u) / 256u) * ((p.m + 255u) / 256u), middle = (u64)((p.n + 127u) / 128u) * ((p.m + 127u) / 128u);
         if (large >= cus * 3 / 4) launch_tiles<T, 8, 4, 2, 4>(p, s);
         else if (middle >= cus * 3 / 4) launch_tiles<T, 4, 4, 2, 2>(p, s);
@@ -254,11 +316,14 @@ void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
 }
 
 void launch_mx_few_rows(const MxProduct &p, u32 cus, hipStream_t s) {
+    const u32 tiles = (p.n + 15u) / 16u;
     with_type(p.x.type, [&](auto xtag) {
         with_type(p.type, [&](auto tag) {
             using X = decltype(xtag);
             using T = decltype(tag);
-            k_mx_few_rows<X, T><<<std::min((p.n + 15u) / 16u, 1u << 20), 256, 0, s>>>(p);
+            if (tiles < 4u * cus) launch_few<X, T, 1, 1>(p, s);
+            else if (tiles < 8u * cus) launch_few<X, T, 2, 1>(p, s);
+            else launch_few<X, T, 4, 1>(p, s);
         });
     });
 }

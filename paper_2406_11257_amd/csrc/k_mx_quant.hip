@@ -1,88 +1,203 @@
 // Microscaled 4-bit floating point: quantisation along the rows and down the columns of a matrix, and back.
+//
+// All three are bound by memory: 2 or 4 bytes an element one way, 0.53 the other.
 #include "excp_ops_device.h"
 
 namespace {
 
 constexpr u32 kThreads = 256;
 
-// One thread a block of 32, element by element.
-template <class T, bool DOWN>
-__global__ __launch_bounds__(kThreads) void k_mx_quantize(const T *__restrict__ x, u64 ld, u32 rows, u32 cols, u32 groups,
-                                                          unsigned char *__restrict__ codes, unsigned char *__restrict__ scales,
-                                                          u64 blocks) {
-    // DOWN: "rows" of codes are the columns of x
-    const u32 lines = DOWN ? cols : rows, len = DOWN ? rows : cols;
-    for (u64 b = blockIdx.x * (u64)kThreads + threadIdx.x; b < blocks; b += (u64)gridDim.x * kThreads) {
-        const u64 per = (u64)groups * 4u;
-        const u32 line = DOWN ? (u32)(b % lines) : (u32)(b / per);
-        const u32 at = DOWN ? (u32)(b / lines) : (u32)(b % per);
-        float v[32];
-        u32 peak = 0;
+// The largest of the quad of lanes that share a block, in all four.
+__device__ __forceinline__ u32 quad_max(u32 v) {
+    v = max(v, dpp_u32<0xb1, 0xf>(v, v));                    // lanes 1 0 3 2
+    return max(v, dpp_u32<0x4e, 0xf>(v, v));                 // lanes 2 3 0 1
+}
+// A group's four scale bytes, one of each quad of its sixteen lanes, in all of them.
+__device__ __forceinline__ u32 group_scales(u32 byte) {
+    u32 v = byte << ((threadIdx.x >> 2 & 3u) * 8u);
+    v |= dpp_u32<0x124, 0xf>(0u, v);                         // rotate the sixteen by 4, by 8
+    return v | dpp_u32<0x128, 0xf>(0u, v);
+}
+
+// Sixteen lanes a group, eight elements each; codes and scales lie group after group, whatever the rows.  A thread has
+// pieces of four groups under way.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_mx_quantize(const T *__restrict__ x, u64 ld, u32 cols, u32 groups, u32 all,
+                                                          unsigned char *__restrict__ codes, unsigned char *__restrict__ scales) {
+    constexpr u32 kPieces = 4, kStep = kThreads / 16u;
+    const u32 at = threadIdx.x & 15u;
+    for (u32 first = blockIdx.x * (kStep * kPieces) + threadIdx.x / 16u; first < all; first += gridDim.x * (kStep * kPieces)) {
+        Eight<T> v[kPieces];
 #pragma unroll
-        for (u32 i = 0; i < 32; ++i) {
-            const u32 j = at * 32u + i;
-            const u64 o = DOWN ? (u64)j * ld + line : (u64)line * ld + j;
-            v[i] = j < len ? widen(x[o]) : 0.0f;
-            peak = max(peak, f2u(v[i]) & 0x7fffffffu);
+        for (u32 q = 0; q < kPieces; ++q) {
+            const u32 i = first + q * kStep, row = i / groups, col = (i - row * groups) * EXCP_MX_GROUP + at * 8u;
+            v[q] = load_eight(x + row * ld + col, i < all && col < cols ? cols - col : 0u);
         }
-        const u32 byte = mx_scale_byte(peak);
-        const float inv = byte == 255u ? 0.0f : mx_inverse(byte);
-        u32 out[4];
 #pragma unroll
-        for (u32 w = 0; w < 4; ++w) {
-            float q[8];
-#pragma unroll
-            for (u32 i = 0; i < 8; ++i) q[i] = byte == 255u ? 0.0f : v[w * 8 + i] * inv;
-            out[w] = mx_codes(q);
+        for (u32 q = 0; q < kPieces; ++q) {
+            const u32 i = first + q * kStep;
+            const u32 byte = mx_scale_byte<T>(quad_max(mx_peak(v[q])));
+            const u32 code = mx_codes(v[q], byte), four = group_scales(byte);
+            if (i >= all) continue;
+            *(u32 *)(codes + i * 64ull + at * 4u) = code;
+            if (at == 0) *(u32 *)(scales + i * 4ull) = four;
         }
-        const u64 o = (u64)line * per + at;
-        *(uint4 *)(codes + o * 16u) = make_uint4(out[0], out[1], out[2], out[3]);
-        scales[o] = (unsigned char)byte;
     }
 }
 
+// A tile of 128 x 128 elements a workgroup: quantised along its rows on the way in, and from LDS down its columns.
+template <class T>
+struct TileRoom {
+    static constexpr u32 pitch = 128 * sizeof(T) / 4 + 1;    // in words
+    u32 word[128 * pitch];
+};
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_mx_quantize_tile(const T *__restrict__ x, u64 ld, u32 rows, u32 cols, u32 tiles_c,
+                                                               unsigned char *__restrict__ codes, unsigned char *__restrict__ scales,
+                                                               unsigned char *__restrict__ codes_t, unsigned char *__restrict__ scales_t) {
+    constexpr u32 kPitch = TileRoom<T>::pitch;
+    __shared__ TileRoom<T> room;
+    const u32 tiles_r = (rows + 127u) / 128u;
+    for (u64 tile = blockIdx.x; tile < (u64)tiles_r * tiles_c; tile += gridDim.x) {
+    const u32 tile_r = (u32)(tile / tiles_c), tile_c = (u32)(tile - (u64)tile_r * tiles_c);
+    const u32 at = threadIdx.x & 15u, col = tile_c * 128u + at * 8u;
+#pragma unroll
+    for (u32 q = 0; q < 8; ++q) {
+        const u32 in = q * 16u + threadIdx.x / 16u, row = tile_r * 128u + in;
+        const Eight<T> v = load_eight(x + (u64)row * ld + col, row < rows && col < cols ? cols - col : 0u);
+        u32 w[8 * sizeof(T) / 4];
+        __builtin_memcpy(w, &v, sizeof w);
+#pragma unroll
+        for (u32 i = 0; i < 8 * sizeof(T) / 4; ++i) room.word[in * kPitch + at * (8 * sizeof(T) / 4) + i] = w[i];
+        if (codes) {                                         // the same for all
+            const u32 byte = mx_scale_byte<T>(quad_max(mx_peak(v)));
+            const u32 code = mx_codes(v, byte), four = group_scales(byte);
+            if (row < rows) {
+                const u64 o = (u64)row * tiles_c + tile_c;
+                *(u32 *)(codes + o * 64u + at * 4u) = code;
+                if (at == 0) *(u32 *)(scales + o * 4u) = four;
+            }
+        }
+    }
+    __syncthreads();
+    // four lanes the four blocks of a column (of two, where a word holds two elements): 64 bytes of codes
+    const u32 block = threadIdx.x & 3u;
+    for (u32 c = threadIdx.x >> 2; c < 128u * sizeof(T) / 4u; c += kThreads / 4u) {
+        const u32 *from = room.word + block * 32u * kPitch + c;
+        u32 v[32];
+#pragma unroll
+        for (u32 i = 0; i < 32; ++i) v[i] = from[i * kPitch];
+        if constexpr (sizeof(T) == 4) {
+            u32 peak = 0, out[4];
+#pragma unroll
+            for (u32 i = 0; i < 32; ++i) peak = max(peak, v[i] & 0x7fffffffu);
+            const u32 byte = mx_scale_byte<T>(peak);
+#pragma unroll
+            for (u32 q = 0; q < 4; ++q) {
+                Eight<T> e;
+                __builtin_memcpy(&e, v + q * 8, sizeof e);
+                out[q] = mx_codes(e, byte);
+            }
+            const u32 j = tile_c * 128u + c;
+            if (j < cols) {
+                const u64 o = (u64)j * tiles_r + tile_r;
+                *(uint4 *)(codes_t + o * 64u + block * 16u) = make_uint4(out[0], out[1], out[2], out[3]);
+                scales_t[o * 4u + block] = (unsigned char)byte;
+            }
+        } else {
+            u32 peaks = 0;
+#pragma unroll
+            for (u32 i = 0; i < 32; ++i) peaks = max_halves(peaks, v[i] & 0x7fff7fffu);
+#pragma unroll
+            for (u32 h = 0; h < 2; ++h) {
+                const u32 byte = mx_scale_byte<T>(h ? peaks >> 16 : peaks & 0xffffu);
+                u32 out[4];
+#pragma unroll
+                for (u32 q = 0; q < 4; ++q) {
+                    u32 w[4];
+#pragma unroll
+                    for (u32 i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(v[q * 8 + i * 2 + 1], v[q * 8 + i * 2], h ? 0x07060302u : 0x05040100u);
+                    Eight<T> e;
+                    __builtin_memcpy(&e, w, sizeof e);
+                    out[q] = mx_codes(e, byte);
+                }
+                const u32 j = tile_c * 128u + c * 2u + h;
+                if (j < cols) {
+                    const u64 o = (u64)j * tiles_r + tile_r;
+                    *(uint4 *)(codes_t + o * 64u + block * 16u) = make_uint4(out[0], out[1], out[2], out[3]);
+                    scales_t[o * 4u + block] = (unsigned char)byte;
+                }
+            }
+        }
+    }
+    __syncthreads();
+    }
+}
+
+// Eight elements a lane.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_mx_dequantize(const unsigned char *__restrict__ codes, const unsigned char *__restrict__ scales,
-                                                            u32 cols, u32 groups, T *__restrict__ x, u64 ld, u64 pieces) {
-    for (u64 i = blockIdx.x * (u64)kThreads + threadIdx.x; i < pieces; i += (u64)gridDim.x * kThreads) {
-        const u64 row = i / (groups * 16u);
-        const u32 at = (u32)(i % (groups * 16u)) * 8u;
-        if (at >= cols) continue;
-        float q[8];
-        mx_values(*(const u32 *)(codes + i * 4u), q);
-        const float scale = mx_power(scales[i / 4u]);
-        T *out = x + row * ld + at;
+                                                            u32 cols, u32 groups, u32 all, T *__restrict__ x, u64 ld) {
+    constexpr u32 kPieces = 4, kStep = kThreads / 16u;
+    const u32 at = threadIdx.x & 15u;
+    for (u32 first = blockIdx.x * (kStep * kPieces) + threadIdx.x / 16u; first < all; first += gridDim.x * (kStep * kPieces)) {
+        u32 code[kPieces], byte[kPieces];
 #pragma unroll
-        for (u32 j = 0; j < 8; ++j)
-            if (at + j < cols) out[j] = (T)(q[j] * scale);
+        for (u32 q = 0; q < kPieces; ++q) {
+            const u32 i = min(first + q * kStep, all - 1u);
+            code[q] = *(const u32 *)(codes + i * 64ull + at * 4u);
+            byte[q] = scales[i * 4ull + at / 4u];
+        }
+#pragma unroll
+        for (u32 q = 0; q < kPieces; ++q) {
+            const u32 i = first + q * kStep, row = i / groups, col = (i - row * groups) * EXCP_MX_GROUP + at * 8u;
+            float v[8];
+            mx_values(code[q], v);
+            const float scale = mx_power(byte[q]);
+            Eight<T> e;
+#pragma unroll
+            for (u32 j = 0; j < 8; ++j) e.v[j] = (T)(v[j] * scale);
+            if (i < all && col < cols) store_eight(x + row * ld + col, e, cols - col);
+        }
     }
 }
 
-u32 grid_for(u64 threads, u32 cus) { return (u32)std::min<u64>((threads + kThreads - 1) / kThreads, (u64)cus * 32u); }
+// Calls f(first row, rows) for parts of a matrix whose groups 31 bits count.
+template <class F>
+void in_parts(u32 rows, u32 groups, F f) {
+    const u32 most = std::max(1u, (1u << 31) / groups);
+    for (u32 r = 0; r < rows; r += std::min(most, rows - r)) f(r, std::min(most, rows - r));
+}
+u32 grid_for(u32 all, u32 cus) { return std::min((all + 63u) / 64u, cus * 16u); }
 
 }  // namespace
 
 void launch_mx_quantize(const MxQuantize &q, u32 cus, hipStream_t s) {
-    with_type(q.x.type, [&](auto tag) {
+    const Matrix &m = q.x;
+    const u32 groups = (m.cols + EXCP_MX_GROUP - 1) / EXCP_MX_GROUP;
+    with_type(m.type, [&](auto tag) {
         using T = decltype(tag);
-        if (q.codes) {
-            const u32 groups = (q.x.cols + EXCP_MX_GROUP - 1) / EXCP_MX_GROUP;
-            const u64 blocks = (u64)q.x.rows * groups * 4u;
-            k_mx_quantize<T, false><<<grid_for(blocks, cus), kThreads, 0, s>>>((const T *)q.x.p, q.x.ld, q.x.rows, q.x.cols, groups, q.codes, q.scales, blocks);
-        }
         if (q.codes_t) {
-            const u32 groups = (q.x.rows + EXCP_MX_GROUP - 1) / EXCP_MX_GROUP;
-            const u64 blocks = (u64)q.x.cols * groups * 4u;
-            k_mx_quantize<T, true><<<grid_for(blocks, cus), kThreads, 0, s>>>((const T *)q.x.p, q.x.ld, q.x.rows, q.x.cols, groups, q.codes_t, q.scales_t, blocks);
+            const u64 tiles = (u64)groups * ((m.rows + 127u) / 128u);
+            k_mx_quantize_tile<T><<<(u32)std::min<u64>(tiles, 1u << 20), kThreads, 0, s>>>((const T *)m.p, m.ld, m.rows, m.cols, groups, q.codes, q.scales, q.codes_t, q.scales_t);
+        } else {
+            in_parts(m.rows, groups, [&](u32 r, u32 rows) {
+                const u32 all = rows * groups;
+                k_mx_quantize<T><<<grid_for(all, cus), kThreads, 0, s>>>((const T *)m.p + (u64)r * m.ld, m.ld, m.cols, groups, all,
+                                                                         q.codes + (u64)r * groups * 64u, q.scales + (u64)r * groups * 4u);
+            });
         }
     });
 }
 
 void launch_mx_dequantize(const MxDequantize &d, u32 cus, hipStream_t s) {
     const u32 groups = (d.cols + EXCP_MX_GROUP - 1) / EXCP_MX_GROUP;
-    const u64 pieces = (u64)d.rows * groups * 16u;
     with_type(d.type, [&](auto tag) {
         using T = decltype(tag);
-        k_mx_dequantize<T><<<grid_for(pieces, cus), kThreads, 0, s>>>(d.codes, d.scales, d.cols, groups, (T *)d.x, d.ld, pieces);
+        in_parts(d.rows, groups, [&](u32 r, u32 rows) {
+            const u32 all = rows * groups;
+            k_mx_dequantize<T><<<grid_for(all, cus), kThreads, 0, s>>>(d.codes + (u64)r * groups * 64u, d.scales + (u64)r * groups * 4u, d.cols, groups,
+                                                                       all, (T *)d.x + (u64)r * d.ld, d.ld);
+        });
     });
 }

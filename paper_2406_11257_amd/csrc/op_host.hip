@@ -69,7 +69,7 @@ int excp_mx_dequantize(excp_ctx *c, const void *codes, const void *scales, uint6
 int excp_mx_matmul(excp_ctx *c, const void *a_codes, const void *a_scales, const void *b_codes, const void *b_scales,
                    uint64_t m, uint64_t n, uint64_t k, void *y, int type, uint64_t ld) {
     u64 size;
-    if (!c || !elem_size(type, size) || !dims_ok(m, n, k)) return EXCP_E_ARG;
+    if (!c || !elem_size(type, size) || !dims_ok(m, n, k) || k > EXCP_MX_MAX_K) return EXCP_E_ARG;
     if (m == 0 || n == 0) return EXCP_OK;
     if (!matrix_ok(y, type, n, ld) || (k && (!coded_ok(a_codes, a_scales) || !coded_ok(b_codes, b_scales)))) return EXCP_E_ARG;
     OpsContext o;
@@ -83,7 +83,7 @@ int excp_mx_matmul(excp_ctx *c, const void *a_codes, const void *a_scales, const
 int excp_mx_linear(excp_ctx *c, const void *x, int x_type, uint64_t ldx, const void *w_codes, const void *w_scales, uint64_t m,
                    uint64_t n, uint64_t k, void *y, int y_type, uint64_t ldy, void *x_codes, void *x_scales) {
     u64 size;
-    if (!c || !elem_size(x_type, size) || !elem_size(y_type, size) || !dims_ok(m, n, k) || !x_codes != !x_scales) return EXCP_E_ARG;
+    if (!c || !elem_size(x_type, size) || !elem_size(y_type, size) || !dims_ok(m, n, k) || k > EXCP_MX_MAX_K || !x_codes != !x_scales) return EXCP_E_ARG;
     if (m == 0 || n == 0) return EXCP_OK;
     if (!matrix_ok(y, y_type, n, ldy)) return EXCP_E_ARG;
     if (k && (!matrix_ok(x, x_type, k, ldx) || !coded_ok(w_codes, w_scales))) return EXCP_E_ARG;

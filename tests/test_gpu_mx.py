@@ -67,18 +67,19 @@ def test_quantize_both_ways_and_back(ctx, rows, cols, dtype, gap, lead):
         assert outside is None or bool((outside == 7.0).all())
 
 
-def test_every_rounding_case():
-    """Around every threshold of the grid, in every octave of the scale that fp32 has, and both signs."""
+@pytest.mark.parametrize("dtype,first", [("f32", -150), ("bf16", -134), ("f16", -25)])
+def test_every_rounding_case(dtype, first):
+    """Around every threshold of the grid, in every octave of the scale that the type has, and both signs."""
     edges = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, 7.75])
-    near = np.concatenate([edges, edges * (1 - 2.0 ** -20), edges * (1 + 2.0 ** -20)])
+    near = np.concatenate([edges, edges * (1 - 2.0 ** {"f32": -20, "bf16": -7, "f16": -10}[dtype]), edges * (1 + 2.0 ** {"f32": -20, "bf16": -7, "f16": -10}[dtype])])
     rows = []
-    for e in range(-150, 126):
+    for e in range(first, {"f32": 126, "bf16": 126, "f16": 14}[dtype]):
         for part in np.array_split(np.concatenate([near, -near]), 3):
             rows.append(np.concatenate([[4.0], part, [0.0, -0.0]])[:32] * 2.0 ** e)
             rows[-1] = np.pad(rows[-1], (0, 32 - len(rows[-1])))
-    a = torch.from_numpy(np.array(rows)).to(torch.float32).double().numpy()
+    a = f64_of_type(np.array(rows), dtype)
     c = X.Context(4096)
-    x = torch.from_numpy(a).float().cuda()
+    x = torch.from_numpy(a).to(DTYPES[dtype]).cuda()
     q = X.mx_empty(len(rows), 32)
     c.excp_mx_quantize(x, *q)
     back = torch.empty_like(x)
@@ -86,7 +87,7 @@ def test_every_rounding_case():
     codes, scales = mx_reference(a)
     assert np.array_equal(q[1].cpu().numpy(), scales)
     assert np.array_equal(q[0].cpu().numpy(), codes)
-    assert np.array_equal(f64(back), mx_values(codes, scales, 32))
+    assert torch.equal(back.cpu(), torch.from_numpy(mx_values(codes, scales, 32)).to(DTYPES[dtype]))
     c.close()
 
 
