@@ -397,7 +397,7 @@ int excp_token_logprobs(excp_ctx *ctx, const void *logits, int type, uint64_t ro
  * from the lse and entropy (needed with g_entropy) that excp_token_logprobs wrote.  Each g may be NULL (zero); targets are
  * needed with g_logprob, top_ids with g_top.  What has no value in a row -- no target, a masked target,
  * index -1 -- takes no part, and a row with nothing unmasked gets zeros.  dlogits has the logits' type and
- * its own ld, and may be the logits' own array (ldd = ld then). */
+ * its own ld, and may be the logits' own array (ldd = ld then; no other overlap). */
 int excp_token_logprobs_backward(excp_ctx *ctx, const void *logits, int type, uint64_t rows, uint64_t vocab,
                                  uint64_t ld, const int64_t *targets, const float *lse, const float *entropy,
                                  const int64_t *top_ids, int ntop, const float *g_logprob, const float *g_entropy,

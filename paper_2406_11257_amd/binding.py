@@ -211,36 +211,44 @@ def excp_decompress_step_static(Wp, blob, blob_bytes, W_recon_out=None, m_out=No
     return rc
 
 
-_types = None
+_types = {}
+_uint8 = _int64 = _float32 = None
+
+
+def _load_types():
+    global _uint8, _int64, _float32
+    import torch
+    _uint8, _int64, _float32 = torch.uint8, torch.int64, torch.float32
+    _types.update({torch.float32: EXCP_TYPE_F32, torch.float16: EXCP_TYPE_F16, torch.bfloat16: EXCP_TYPE_BF16})
 
 
 def _type_of(t, name, device):
     """EXCP_TYPE_* of a matrix on the context's device whose rows are contiguous."""
-    global _types
-    if _types is None:
-        import torch
-        _types = {torch.float32: EXCP_TYPE_F32, torch.float16: EXCP_TYPE_F16, torch.bfloat16: EXCP_TYPE_BF16}
     kind = _types.get(t.dtype)
     if kind is None or t.dim() != 2 or t.device != device or (t.stride(1) != 1 and t.shape[1] > 1):
         raise TypeError(f"{name} must be a float32, float16 or bfloat16 matrix on {device} with contiguous rows")
     return kind
 
 
-def _ld(t):
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _ld(t, rows, cols):
+    return t.stride(0) if rows > 1 else cols
 
 
 def _check_vec(t, name, dtype, shape, device):
-    if t is None or t.dtype != dtype or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
+    if t is None or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device}")
+    return t.data_ptr()
+
+
+def _opt_vec(t, name, dtype, shape, device):
+    return None if t is None else _check_vec(t, name, dtype, shape, device)
 
 
 def _check_coded(codes, scales, rows, cols, name, device):
     """Codes and scales of a rows x cols matrix, as mx_empty makes them."""
-    import torch
     groups = (cols + 127) // 128
-    _check_vec(codes, name + " codes", torch.uint8, (rows, groups * 64), device)
-    _check_vec(scales, name + " scales", torch.uint8, (rows, groups * 4), device)
+    return (_check_vec(codes, name + " codes", _uint8, (rows, groups * 64), device),
+            _check_vec(scales, name + " scales", _uint8, (rows, groups * 4), device))
 
 
 def mx_empty(rows: int, cols: int, device="cuda"):
@@ -266,6 +274,7 @@ class Context:
 
     def __init__(self, max_tensor_elems: int, max_group_elems: int | None = None, device=None, stream=None):
         import torch
+        _load_types()
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
@@ -486,89 +495,77 @@ class Context:
     def excp_mx_quantize(self, x, codes=None, scales=None, codes_t=None, scales_t=None):
         """x (a matrix) into codes and scales of its rows, and (or) of its columns: tensors as mx_empty makes them for
         x's shape and for its transpose's."""
-        kind, (rows, cols) = _type_of(x, "x", self.device), x.shape
-        if codes is not None:
-            _check_coded(codes, scales, rows, cols, "the rows'", self.device)
-        if codes_t is not None:
-            _check_coded(codes_t, scales_t, cols, rows, "the columns'", self.device)
-        rc = lib().excp_mx_quantize(self._h, x.data_ptr(), kind, rows, cols, _ld(x),
-                                    *[None if t is None else t.data_ptr() for t in (codes, scales, codes_t, scales_t)])
+        device, kind, (rows, cols) = self.device, _type_of(x, "x", self.device), x.shape
+        c, s = (None, None) if codes is None else _check_coded(codes, scales, rows, cols, "the rows'", device)
+        ct, st = (None, None) if codes_t is None else _check_coded(codes_t, scales_t, cols, rows, "the columns'", device)
+        rc = lib().excp_mx_quantize(self._h, x.data_ptr(), kind, rows, cols, _ld(x, rows, cols), c, s, ct, st)
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_mx_quantize")
 
     def excp_mx_dequantize(self, codes, scales, x):
         """The values of codes and scales into the matrix x."""
         kind, (rows, cols) = _type_of(x, "x", self.device), x.shape
-        _check_coded(codes, scales, rows, cols, "x's", self.device)
-        rc = lib().excp_mx_dequantize(self._h, codes.data_ptr(), scales.data_ptr(), rows, cols, x.data_ptr(), kind, _ld(x))
+        c, s = _check_coded(codes, scales, rows, cols, "x's", self.device)
+        rc = lib().excp_mx_dequantize(self._h, c, s, rows, cols, x.data_ptr(), kind, _ld(x, rows, cols))
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_mx_dequantize")
 
     def excp_mx_matmul(self, a_codes, a_scales, b_codes, b_scales, k, y):
         """y (m x n) = A B^T of A (m x k) and B (n x k) in codes and scales."""
-        kind, (m, n) = _type_of(y, "y", self.device), y.shape
-        _check_coded(a_codes, a_scales, m, k, "A's", self.device)
-        _check_coded(b_codes, b_scales, n, k, "B's", self.device)
-        rc = lib().excp_mx_matmul(self._h, a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(),
-                                  m, n, k, y.data_ptr(), kind, _ld(y))
+        device, kind, (m, n) = self.device, _type_of(y, "y", self.device), y.shape
+        a, sa = _check_coded(a_codes, a_scales, m, k, "A's", device)
+        b, sb = _check_coded(b_codes, b_scales, n, k, "B's", device)
+        rc = lib().excp_mx_matmul(self._h, a, sa, b, sb, m, n, k, y.data_ptr(), kind, _ld(y, m, n))
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_mx_matmul")
 
     def excp_mx_linear(self, x, w_codes, w_scales, y, x_codes=None, x_scales=None):
         """y (m x n) = MX(x) W^T; x_codes and x_scales (as mx_empty makes them for x) are room to work in, not needed
         for up to EXCP_MX_FEW_ROWS rows."""
-        kind, (m, k) = _type_of(x, "x", self.device), x.shape
-        ykind, n = _type_of(y, "y", self.device), y.shape[1]
-        if y.shape[0] != m:
+        device, kind, (m, k) = self.device, _type_of(x, "x", self.device), x.shape
+        ykind, (my, n) = _type_of(y, "y", device), y.shape
+        if my != m:
             raise ValueError("x and y differ in rows")
-        _check_coded(w_codes, w_scales, n, k, "W's", self.device)
-        if x_codes is not None:
-            _check_coded(x_codes, x_scales, m, k, "x's", self.device)
-        rc = lib().excp_mx_linear(self._h, x.data_ptr(), kind, _ld(x), w_codes.data_ptr(), w_scales.data_ptr(), m, n, k,
-                                  y.data_ptr(), ykind, _ld(y), None if x_codes is None else x_codes.data_ptr(),
-                                  None if x_scales is None else x_scales.data_ptr())
+        w, sw = _check_coded(w_codes, w_scales, n, k, "W's", device)
+        c, s = (None, None) if x_codes is None else _check_coded(x_codes, x_scales, m, k, "x's", device)
+        rc = lib().excp_mx_linear(self._h, x.data_ptr(), kind, _ld(x, m, k), w, sw, m, n, k, y.data_ptr(), ykind, _ld(y, m, n), c, s)
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_mx_linear")
 
     # -- log probabilities of tokens -------------------------------------------------------
     def excp_token_logprobs(self, logits, targets=None, logprob=None, entropy=None, lse=None, top_logprob=None, top_ids=None):
         """Statistics of every row of logits into the tensors given: logprob of the row's target and entropy (float32,
-        one a row), lse in two parts to be added (float32, rows x 2), the largest log probabilities and their indices (float32 and int64, rows x ntop)."""
-        import torch
-        kind, (rows, vocab) = _type_of(logits, "logits", self.device), logits.shape
-        ntop = 0
-        for t, nm, dtype in ((top_logprob, "top_logprob", torch.float32), (top_ids, "top_ids", torch.int64)):
-            if t is not None:
-                ntop = t.shape[-1] if ntop == 0 else ntop
-                _check_vec(t, nm, dtype, (rows, ntop), self.device)
-        for t, nm, dtype, shape in ((targets, "targets", torch.int64, (rows,)), (logprob, "logprob", torch.float32, (rows,)),
-                                    (entropy, "entropy", torch.float32, (rows,)), (lse, "lse", torch.float32, (rows, 2))):
-            if t is not None:
-                _check_vec(t, nm, dtype, shape, self.device)
-        rc = lib().excp_token_logprobs(self._h, logits.data_ptr(), kind, rows, vocab, _ld(logits),
-                                       None if targets is None else targets.data_ptr(), ntop,
-                                       *[None if t is None else t.data_ptr() for t in (logprob, entropy, lse, top_logprob, top_ids)])
+        one a row), lse in two parts to be added (float32, rows x 2), the largest log probabilities and their indices
+        (float32 and int64, rows x ntop)."""
+        device, kind, (rows, vocab) = self.device, _type_of(logits, "logits", self.device), logits.shape
+        top = top_ids if top_logprob is None else top_logprob
+        ntop = 0 if top is None else top.shape[-1]
+        rc = lib().excp_token_logprobs(self._h, logits.data_ptr(), kind, rows, vocab, _ld(logits, rows, vocab),
+                                       _opt_vec(targets, "targets", _int64, (rows,), device), ntop,
+                                       _opt_vec(logprob, "logprob", _float32, (rows,), device),
+                                       _opt_vec(entropy, "entropy", _float32, (rows,), device),
+                                       _opt_vec(lse, "lse", _float32, (rows, 2), device),
+                                       _opt_vec(top_logprob, "top_logprob", _float32, (rows, ntop), device),
+                                       _opt_vec(top_ids, "top_ids", _int64, (rows, ntop), device))
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_token_logprobs")
 
     def excp_token_logprobs_backward(self, logits, targets, lse, entropy, top_ids, g_logprob, g_entropy, g_top, dlogits):
         """The gradient over the logits, into dlogits (which may be the logits), from what excp_token_logprobs wrote;
         each g may be None."""
-        import torch
-        kind, (rows, vocab) = _type_of(logits, "logits", self.device), logits.shape
-        if _type_of(dlogits, "dlogits", self.device) != kind or dlogits.shape != logits.shape:
+        device, kind, (rows, vocab) = self.device, _type_of(logits, "logits", self.device), logits.shape
+        if _type_of(dlogits, "dlogits", device) != kind or dlogits.shape != logits.shape:
             raise TypeError("dlogits must have the logits' type and shape")
         ntop = 0 if g_top is None else g_top.shape[-1]
-        for t, nm, dtype, shape in ((targets, "targets", torch.int64, (rows,)), (lse, "lse", torch.float32, (rows, 2)),
-                                    (entropy, "entropy", torch.float32, (rows,)), (g_logprob, "g_logprob", torch.float32, (rows,)),
-                                    (g_entropy, "g_entropy", torch.float32, (rows,)), (g_top, "g_top", torch.float32, (rows, ntop))):
-            if t is not None:
-                _check_vec(t, nm, dtype, shape, self.device)
-        if g_top is not None and top_ids is not None:
-            _check_vec(top_ids, "top_ids", torch.int64, (rows, ntop), self.device)
-        ptr = [None if t is None else t.data_ptr() for t in (targets, lse, entropy, top_ids, g_logprob, g_entropy, g_top)]
-        rc = lib().excp_token_logprobs_backward(self._h, logits.data_ptr(), kind, rows, vocab, _ld(logits), *ptr[:4], ntop,
-                                                *ptr[4:], dlogits.data_ptr(), _ld(dlogits))
+        rc = lib().excp_token_logprobs_backward(self._h, logits.data_ptr(), kind, rows, vocab, _ld(logits, rows, vocab),
+                                                _opt_vec(targets, "targets", _int64, (rows,), device),
+                                                _opt_vec(lse, "lse", _float32, (rows, 2), device),
+                                                _opt_vec(entropy, "entropy", _float32, (rows,), device),
+                                                _opt_vec(top_ids, "top_ids", _int64, (rows, ntop), device) if ntop else None, ntop,
+                                                _opt_vec(g_logprob, "g_logprob", _float32, (rows,), device),
+                                                _opt_vec(g_entropy, "g_entropy", _float32, (rows,), device),
+                                                _opt_vec(g_top, "g_top", _float32, (rows, ntop), device),
+                                                dlogits.data_ptr(), _ld(dlogits, rows, vocab))
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_token_logprobs_backward")
 

@@ -53,7 +53,7 @@ struct excp_ctx {
     // descriptors and tile tables of a call, one after the other (see Staged): pinned, and the device's copy
     unsigned char *h_stage = nullptr, *d_stage = nullptr;
     HostRec *h_rec = nullptr;
-    struct RowPart *row_parts = nullptr;     // of the operators on rows of logits (see excp_ops.h)
+    RowPart *row_parts = nullptr;     // of the operators on rows of logits (see excp_ops.h)
     u32 *row_tickets = nullptr;
     u64 ws_bytes = 0;
     std::vector<void *> allocs;
@@ -407,6 +407,7 @@ int excp_create(excp_ctx **out, int hip_device, void *hip_stream, uint64_t max_t
     ok = ok && dev_alloc(c, &w.dec_kinds, 4);
     w.dec_part_stride = excp_scan_runs(kMaxBatchTensors, (u32)std::min<u64>(max_tiles * EXCP_MAX_CHAIN, 0xffffffffull - EXCP_SCAN_TILES));
     ok = ok && dev_alloc(c, &w.dec_part, 2ull * w.dec_part_stride);
+    ok = ok && dev_alloc(c, &c->row_parts, EXCP_ROW_PARTS) && dev_alloc(c, &c->row_tickets, EXCP_ROW_PARTS);
     if (ok) {
         // (the kernels write the results where the host reads them: no copy back)
         ok = hipHostMalloc((void **)&c->h_stage, kStageBytes) == hipSuccess &&
@@ -426,6 +427,7 @@ int excp_create(excp_ctx **out, int hip_device, void *hip_stream, uint64_t max_t
         launch_zero_u32(w.med_hist, (u64)kMaxGroupTensors * 2048, c->stream);
         launch_zero_u32(w.sel_ticket, kMaxGroupTensors, c->stream);
         launch_zero_u32(w.scan_ticket, 1, c->stream);
+        launch_zero_u32(c->row_tickets, EXCP_ROW_PARTS, c->stream);
         launch_zero_u32(w.dec_kinds, 4, c->stream);
         ok = hipStreamSynchronize(c->stream) == hipSuccess;
     }

@@ -5,12 +5,17 @@
 
 struct excp_ctx;
 
+#define EXCP_TOP_MAX 64u           // alternatives of a row (EXCP_MAX_TOP of the C ABI)
+#define EXCP_ROW_PARTS 1024u       // parts of rows that a call may have
+// What one workgroup found in its part of a row of logits (see k_logprobs.hip).
+struct RowPart { float max, sum, weighted, pad; u64 key[EXCP_TOP_MAX]; };
+
 // What an operator needs of a context.
 struct OpsContext {
     int device;
     hipStream_t stream;
     u32 cus;               // compute units
-    struct RowPart *parts; // EXCP_ROW_PARTS records of rows that several workgroups share
+    RowPart *parts;        // EXCP_ROW_PARTS records of rows that several workgroups share
     u32 *tickets;          // as many counters, zero between calls
     bool broken;
 };

@@ -16,12 +16,18 @@ __device__ __forceinline__ float widen(__bf16 x) { return (float)x; }
 // Eight consecutive elements, as they are stored: 16 B of a 16-bit type, 32 B of floats.
 template <class T> struct Eight { T v[8]; };
 
-// The first `have` of eight elements, zeros after them.  (Whole ones in pieces of 16 bytes, wherever they begin.)
+// The first `have` of eight elements, zeros after them.  Whole ones in pieces of 16 bytes, wherever they begin.  (As vectors of
+// words: where both ways move elements, the compiler joins what they have in common, and pieces of 12 bytes and less are left.)
+typedef unsigned int words_anywhere __attribute__((ext_vector_type(4), aligned(2)));
 template <class T>
 __device__ __forceinline__ Eight<T> load_eight(const T *p, u32 have) {
     Eight<T> r;
     if (have >= 8u) {
-        __builtin_memcpy(&r, p, sizeof r);
+        const auto *from = (const words_anywhere *)p;
+        v4u32 w[sizeof r / 16];
+#pragma unroll
+        for (u32 i = 0; i < sizeof r / 16; ++i) w[i] = from[i];
+        __builtin_memcpy(&r, w, sizeof r);
     } else {
 #pragma unroll
         for (u32 i = 0; i < 8; ++i) r.v[i] = i < have ? p[i] : (T)0;
@@ -31,7 +37,11 @@ __device__ __forceinline__ Eight<T> load_eight(const T *p, u32 have) {
 template <class T>
 __device__ __forceinline__ void store_eight(T *p, const Eight<T> &r, u32 have) {
     if (have >= 8u) {
-        __builtin_memcpy(p, &r, sizeof r);
+        auto *to = (words_anywhere *)p;
+        v4u32 w[sizeof r / 16];
+        __builtin_memcpy(w, &r, sizeof r);
+#pragma unroll
+        for (u32 i = 0; i < sizeof r / 16; ++i) to[i] = w[i];
     } else {
 #pragma unroll
         for (u32 i = 0; i < 8; ++i)

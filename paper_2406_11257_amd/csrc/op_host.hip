@@ -6,6 +6,8 @@
 
 namespace {
 
+static_assert(EXCP_TOP_MAX == EXCP_MAX_TOP, "");
+
 bool elem_size(int type, u64 &size) {
     switch (type) {
         case EXCP_TYPE_F32: size = 4; return true;

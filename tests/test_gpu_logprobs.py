@@ -140,6 +140,29 @@ def test_ties_and_what_is_no_number(ctx, dtype, vocab):
     assert (np.abs(f64(d) - ref)[fin] <= 1e-4 + HALF_ULP[dtype] * np.abs(ref[fin])).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_in_place_with_masked_targets(ctx, dtype):
+    """In place, whether a target is masked is found out before its logit is overwritten: long rows, several chunks."""
+    rows, vocab = 600, 70001
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    logits = torch.empty(rows, vocab, device="cuda").normal_(0, 2, generator=g).to(DTYPES[dtype])
+    targets = torch.randint(0, vocab, (rows,), device="cuda", generator=g)
+    logits[torch.arange(rows, device="cuda")[::2], targets[::2]] = -float("inf")
+    o = outputs(rows, 4)
+    ctx.excp_token_logprobs(logits, targets, **o)
+    gl, gt = torch.ones(rows, device="cuda"), torch.full((rows, 4), 0.5, device="cuda")
+    d = torch.empty_like(logits)
+    ctx.excp_token_logprobs_backward(logits, targets, o["lse"], None, o["top_ids"], gl, None, gt, d)
+    ctx.excp_token_logprobs_backward(logits, targets, o["lse"], None, o["top_ids"], gl, None, gt, logits)
+    assert torch.equal(d, logits)
+    # the weights of a row sum to zero but for what a type rounds: 2^-8 of sum |d| < 2 (1 + 4 / 2)
+    assert bool((d.double().sum(1).abs() < {"f32": 1e-4, "bf16": 6 * 2.0 ** -8}[dtype]).all())
+    assert bool((o["logprob"][::2] == -float("inf")).all())
+    at = d.gather(1, targets[:, None])[:, 0]
+    assert bool((at[::2] == 0).all()) and bool((at[1::2] > 0.1).all())
+
+
 @pytest.mark.parametrize("which", ["logprob", "entropy", "top"])
 def test_gradient_against_differences(ctx, which):
     """Central differences of the fp32 outputs' 64-bit counterparts, in every direction of a small row."""
