@@ -3,6 +3,8 @@
 // Both passes are bound by memory: the first reads a row once, the second reads and writes it once.
 #include "excp_ops_device.h"
 
+#include <type_traits>
+
 namespace {
 
 constexpr u32 kThreads = 256, kWaves = kThreads / 64u;
@@ -53,54 +55,103 @@ __device__ __forceinline__ u32 key_index(u64 key) { return ~(u32)key; }
 
 struct Room {
     Sums sums[kWaves];
-    u32 group[64], owner[kThreads];
-    u64 key[kThreads], candidate[kCandidates], best[kWaves], least;
-    u32 thread[EXCP_TOP_MAX], keys, candidates;
+    u32 value[kThreads], owner[kThreads], where[kThreads];
+    u64 candidate[kCandidates], best[kWaves];
+    u32 owners, candidates;
 };
 
+// The largest bound that at least k of a wave's R numbers a lane reach, or one that k reach exactly; 0 where fewer than k are
+// not 0.  Bit by bit, from the highest in which the numbers' upper words (a 32-bit number's own) differ.
+template <class N> __device__ __forceinline__ u32 upper_word(N v) { return (u32)(v >> (8 * sizeof(N) - 32)); }
+// (Not below bit `last`: where the numbers have nothing there.)
+template <int R, class N>
+__device__ __forceinline__ N bound_of(const N (&v)[R], u32 k, int last = 0) {
+    u32 most = 0, least = ~0u;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        most = max(most, upper_word(v[r]));
+        least = min(least, upper_word(v[r]));
+    }
+    most = wave_max_u32(most);
+    const u32 differ = most ^ wave_min_u32(least);
+    const int below = 8 * (int)sizeof(N) - 32, high = differ ? 31 - __builtin_clz(differ) : -1;
+    N t = high == 31 ? 0 : (N)(most >> (high + 1)) << (high + 1 + below);
+    for (int b = high + below; b >= last; --b) {
+        const N c = t | (N)1 << b;
+        u32 n = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) n += (u32)__popcll(ballot64(v[r] >= c));
+        if (n >= k) t = c;
+        if (n == k) break;                                   // the same in every lane
+    }
+    return t;
+}
 // Number of `keys` above `key`.
 __device__ __forceinline__ u32 above(const u64 *keys, u32 count, u64 key) {
     u32 n = 0;
-#pragma unroll 8
+#pragma unroll 4
     for (u32 i = 0; i < count; ++i) n += keys[i] > key;
     return n;
 }
-// put(place, key) for the `ntop` first of `count` keys, no two alike but zeros (what is none), and put(place, 0) for places
-// that none takes.
-template <class Put>
-__device__ void rank_all(const u64 *keys, u32 count, int ntop, Put put) {
-    u32 some = 0;
-    for (u32 i = threadIdx.x; i - threadIdx.x < count; i += kThreads) {
-        const u64 key = i < count ? keys[i] : 0;
-        some += (u32)__syncthreads_count(key != 0);
-        const u32 rank = key ? above(keys, count, key) : ~0u;
-        if (rank < (u32)ntop) put(rank, key);
+// The k (at most 64) first of `count` keys in LDS, no two alike: one a lane with its place among them, 0 in the other lanes.
+// One wave; the keys are overwritten.
+struct Placed { u64 key; u32 place; };
+template <int R>
+__device__ __forceinline__ u32 keep_first(u64 *keys, u32 count, u32 k) {
+    const u32 lane = lane_id();
+    u64 v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = r * 64u + lane < count ? keys[r * 64u + lane] : 0;
+    const u64 least = max(bound_of(v, k), (u64)1);
+    u32 n = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const u64 in = ballot64(v[r] >= least);
+        if (v[r] >= least) keys[n + lanes_below(in)] = v[r];
+        n += (u32)__popcll(in);
     }
-    if (threadIdx.x >= some && threadIdx.x < (u32)ntop) put(threadIdx.x, 0);
+    wave_lds_fence();
+    return n;
 }
-static_assert(EXCP_TOP_MAX <= 64, "one wave writes a row's alternatives");
+__device__ __forceinline__ Placed first_of(u64 *keys, u32 count, u32 k) {
+    wave_lds_fence();
+    if (count > 256u) count = keep_first<kCandidates / 64>(keys, count, k);
+    else if (count > 64u) count = keep_first<4>(keys, count, k);
+    Placed r = {lane_id() < count ? keys[lane_id()] : 0, 0};
+    r.place = above(keys, count, r.key);
+    if (r.place >= k) r.key = 0;
+    return r;
+}
+static_assert(EXCP_TOP_MAX <= 64, "a row's alternatives are one wave's");
 
-// Statistics of pieces [begin, end) of eight elements of a row, in the first wave; and its `ntop` first alternatives by
-// put(place, key).
+// Statistics of pieces [begin, end) of eight elements of a row, in the first wave; and there, in `top`, its `ntop` first
+// alternatives (key 0: none).
 //
-// Every thread keeps the largest of the logits that it has seen and the piece that held it.  The row's first ntop
-// alternatives are all among the logits of the ntop threads whose largest ones come first: before one in another thread
-// would come those ntop.  So only those threads' pieces are read again, out of the caches, and of them only what does not
-// come after the last of those ntop is ranked.
-template <class T, class Put>
-__device__ Sums row_part(const T *x, u32 vocab, u32 begin, u32 end, int ntop, Room &room, Put put) {
+// Every thread keeps the piece that holds the largest of the logits that it has seen, and the largest of any other piece.  If
+// ntop threads, or groups of threads, have seen a logit of at least b, then ntop logits are at least b, and what is below b is
+// no alternative.  Groups of four threads give a bound that is little worse where alternatives are few beside them.  What
+// reaches the bound is a candidate: out of the pieces kept, and where another piece of a thread has reached it too, out of all
+// of its pieces, read again.
+template <bool TOP, class T>
+__device__ Sums row_part(const T *x, u32 vocab, u32 begin, u32 end, int ntop, Room &room, Placed &top) {
     constexpr u32 kUnroll = sizeof(T) == 2 ? 4 : 2;
     const u32 tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
     Sums a = {-INFINITY, 0.0f, 0.0f};
+    Eight<T> kept = {};
+    float second = -INFINITY;
     u32 where = 0;
     auto take = [&](const Eight<T> &e, u32 piece) __attribute__((always_inline)) {
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = widen(e.v[i]);
         const float most = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+        if constexpr (TOP) second = fmaxf(second, fminf(most, a.max));
         if (most > a.max) {
             lower(a, most);
-            where = piece;
+            if constexpr (TOP) {
+                kept = e;
+                where = piece;
+            }
         }
         const float shift = fmaxf(a.max, kLowest);
 #pragma unroll
@@ -133,26 +184,19 @@ __device__ Sums row_part(const T *x, u32 vocab, u32 begin, u32 end, int ntop, Ro
     a.sum = wave_sum_f32(a.sum);
     a.weighted = wave_sum_f32(a.weighted);
     if (lane == 0) room.sums[wave] = a;
-    // A bound for the threads' largest logits: of those of groups of threads the one at place ntop.
-    const u64 key = ntop ? rank_key(mine, where) : 0;
-    const bool small = ntop <= 8;                            // (groups of sixteen lanes, sixteen groups: a quarter of the comparisons)
-    if (ntop) {
-        u32 v = (u32)(key >> 32);
-        v = max(v, dpp_u32<0xb1, 0xf>(v, v));                // the other three of four lanes
-        v = max(v, dpp_u32<0x4e, 0xf>(v, v));
-        if (small) {
-            v = max(v, dpp_u32<0x124, 0xf>(v, v));           // and of sixteen
-            v = max(v, dpp_u32<0x128, 0xf>(v, v));
-            if ((lane & 15u) == 0) room.group[tid >> 4] = v;
-        } else if ((lane & 3u) == 0) {
-            room.group[tid >> 2] = v;
+    const u32 value = TOP ? (u32)(rank_key(mine, 0) >> 32) : 0u;
+    const bool quads = ntop <= 24;
+    constexpr int kLastBit = std::is_same<T, float>::value ? 0 : std::is_same<T, __bf16>::value ? 16 : 13;
+    if (TOP) {
+        u32 v = value;
+        if (quads) {
+            v = max(v, dpp_u32<0xb1, 0xf>(v, v));
+            v = max(v, dpp_u32<0x4e, 0xf>(v, v));
+            if ((lane & 3u) == 0) room.value[tid >> 2] = v;
+        } else {
+            room.value[tid] = v;
         }
-        if (tid < (u32)ntop) room.thread[tid] = ~0u;
-        if (tid == 0) {
-            room.keys = 0;
-            room.candidates = 0;
-            room.least = 1;
-        }
+        if (tid == 0) room.owners = room.candidates = 0;
     }
     __syncthreads();
     Sums all = room.sums[0];
@@ -167,56 +211,52 @@ __device__ Sums row_part(const T *x, u32 vocab, u32 begin, u32 end, int ntop, Ro
             all.weighted += b.weighted;
         }
     }
-    if (!ntop) return all;
-    const u32 groups = small ? 16u : 64u, group = lane < groups ? room.group[lane] : 0u;
-    u32 place = 0;
-#pragma unroll 4
-    for (u32 i = 0; i < groups; ++i) {
-        const u32 v = room.group[i];
-        place += v > group || (v == group && i < lane);
-    }
-    const u64 holds = ballot64(lane < groups && place == (u32)ntop - 1u);
-    const u32 bound = max(1u, (u32)__builtin_amdgcn_readlane((int)group, (int)__ffsll((long long)holds) - 1));
-    const bool is_key = (u32)(key >> 32) >= bound;
-    const u64 with = ballot64(is_key);
-    if (with) {
-        u32 at = 0;
-        if (lane == 0) at = atomicAdd(&room.keys, (u32)__popcll(with));
-        at = (u32)__builtin_amdgcn_readfirstlane((int)at) + lanes_below(with);
-        if (is_key) {
-            room.key[at] = key;
-            room.owner[at] = tid;
-        }
-    }
-    __syncthreads();
-    const u32 keys = room.keys;
-    if (tid < keys) {
-        const u64 k = room.key[tid];
-        const u32 rank = above(room.key, keys, k);
-        if (rank < (u32)ntop) room.thread[rank] = room.owner[tid];
-        if (rank == (u32)ntop - 1u) room.least = k & ~0xffffffffull;            // its value; the piece's number is no index
-    }
-    __syncthreads();
-    // what may be among the first, of the pieces of those threads
-    const u64 least = room.least;
-    const u32 steps = (end - begin + kThreads - 1u) / kThreads;
-    for (u32 i = tid; i < steps * (u32)ntop; i += kThreads) {
-        const u32 who = room.thread[i % (u32)ntop], p = begin + who + i / (u32)ntop * kThreads;
-        if (who == ~0u || p >= end) continue;
-        const Eight<T> e = load_eight(x + (u64)p * 8u, vocab - p * 8u);
+    top = {0, 0};
+    if (!TOP) return all;
+    u32 v[4] = {room.value[lane], 0u, 0u, 0u}, bound;
+    if (quads) {
+        const u32 one[1] = {v[0]};
+        bound = bound_of(one, (u32)ntop, kLastBit);
+    } else {
 #pragma unroll
-        for (u32 j = 0; j < 8; ++j) {
-            const u64 k = p * 8u + j < vocab ? rank_key(widen(e.v[j]), p * 8u + j) : 0;
-            if (k >= least) {
-                const u32 at = atomicAdd(&room.candidates, 1u);
-                if (at < kCandidates) room.candidate[at] = k;
+        for (u32 r = 1; r < 4; ++r) v[r] = room.value[r * 64u + lane];
+        bound = bound_of(v, (u32)ntop, kLastBit);
+    }
+    bound = max(bound, 1u);
+    const float reach = bound > 1u ? key_value((u64)bound << 32) : kLowest;
+    auto add = [&](const Eight<T> &e, u32 piece) __attribute__((always_inline)) {
+        u32 hits = 0;
+#pragma unroll
+        for (u32 j = 0; j < 8; ++j) hits |= (piece * 8u + j < vocab && widen(e.v[j]) >= reach ? 1u : 0u) << j;
+        if (hits == 0u) return;
+        u32 at = atomicAdd(&room.candidates, (u32)__builtin_popcount(hits));
+#pragma unroll
+        for (u32 j = 0; j < 8; ++j)
+            if (hits >> j & 1u) {
+                if (at < kCandidates) room.candidate[at] = rank_key(widen(e.v[j]), piece * 8u + j);
+                ++at;
             }
+    };
+    if (value >= bound) {
+        add(kept, where);
+        if (second >= reach) {
+            const u32 at = atomicAdd(&room.owners, 1u);
+            room.owner[at] = tid;
+            room.where[at] = where;
         }
     }
     __syncthreads();
+    const u32 owners = room.owners, steps = (end - begin + kThreads - 1u) / kThreads;
+    if (owners) {
+        for (u32 i = tid; i < steps * owners; i += kThreads) {
+            const u32 o = i % owners, p = begin + room.owner[o] + i / owners * kThreads;
+            if (p < end && p != room.where[o]) add(load_eight(x + (u64)p * 8u, vocab - p * 8u), p);
+        }
+        __syncthreads();
+    }
     const u32 count = room.candidates;
     if (count <= kCandidates) {
-        rank_all(room.candidate, count, ntop, put);
+        if (wave == 0) top = first_of(room.candidate, count, (u32)ntop);
     } else {
         // too many for that (logits that are tied, or laid out so that a few threads hold all large ones): one after another
         u64 last = ~0ull;
@@ -235,7 +275,7 @@ __device__ Sums row_part(const T *x, u32 vocab, u32 begin, u32 end, int ntop, Ro
             __syncthreads();
             next = max(max(room.best[0], room.best[1]), max(room.best[2], room.best[3]));
             __syncthreads();
-            if (tid == 0) put((u32)j, next);
+            if (lane == (u32)j) top = {next, (u32)j};
             last = next;
         }
     }
@@ -268,33 +308,43 @@ __device__ __forceinline__ void write_top(const RowScores &p, u32 row, u32 place
     if (p.top_logprob) p.top_logprob[o] = !(a.sum == a.sum) ? NAN : key ? (key_value(key) - a.max) - logf(a.sum) : -INFINITY;
 }
 
+// The first wave's alternatives, one a lane, and the places that none takes.
+__device__ __forceinline__ void write_tops(const RowScores &p, u32 row, const Placed &top, const Sums &a) {
+    const u32 lane = lane_id(), some = (u32)__popcll(ballot64(top.key != 0));
+    if (top.key) write_top(p, row, top.place, top.key, a);
+    if (lane >= some && lane < (u32)p.ntop) write_top(p, row, lane, 0, a);
+}
+
 // A workgroup a row.
-template <class T>
+template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_row_scores(const RowScores p) {
     __shared__ Room room;
-    __shared__ u64 first[EXCP_TOP_MAX];
     for (u32 row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const T *x = (const T *)p.logits + (u64)row * p.ld;
-        const Sums a = row_part(x, p.vocab, 0u, (p.vocab + 7u) / 8u, p.ntop, room, [&](u32 place, u64 key) { first[place] = key; });
+        Placed top;
+        const Sums a = row_part<TOP>(x, p.vocab, 0u, (p.vocab + 7u) / 8u, p.ntop, room, top);
         if (threadIdx.x == 0) write_row(p, row, x, a);
-        __syncthreads();
-        for (u32 i = threadIdx.x; i < (u32)p.ntop; i += kThreads) write_top(p, row, i, first[i], a);
+        if (TOP && threadIdx.x < 64u) write_tops(p, row, top, a);
         __syncthreads();
     }
 }
 
 // Few rows: `parts` workgroups a row.  The last of a row's to finish, by ticket, joins what they found.  (Parts pass through
 // memory as relaxed atomics of the device, which have arrived before the ticket is drawn.)
-template <class T>
+template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void k_row_scores_split(const RowScores p, u32 parts, u32 per, RowPart *__restrict__ out, u32 *__restrict__ tickets) {
     __shared__ Room room;
     __shared__ u32 ticket;
     const u32 row = blockIdx.x / parts, part = blockIdx.x - row * parts, all = (p.vocab + 7u) / 8u;
     const T *x = (const T *)p.logits + (u64)row * p.ld;
     RowPart &mine = out[blockIdx.x];
-    const Sums a = row_part(x, p.vocab, min(part * per, all), min(part * per + per, all), p.ntop, room, [&](u32 place, u64 key) {
-        __hip_atomic_store(&mine.key[place], key, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    });
+    Placed top;
+    const Sums a = row_part<TOP>(x, p.vocab, min(part * per, all), min(part * per + per, all), p.ntop, room, top);
+    if (TOP && threadIdx.x < 64u) {
+        const u32 lane = lane_id(), some = (u32)__popcll(ballot64(top.key != 0));
+        if (top.key) __hip_atomic_store(&mine.key[top.place], top.key, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (lane >= some && lane < (u32)p.ntop) __hip_atomic_store(&mine.key[lane], (u64)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     if (threadIdx.x == 0) {
         __hip_atomic_store(&mine.max, a.max, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __hip_atomic_store(&mine.sum, a.sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -318,18 +368,20 @@ __global__ __launch_bounds__(kThreads) void k_row_scores_split(const RowScores p
     b.sum = wave_sum_f32(b.sum);
     b.weighted = wave_sum_f32(b.weighted);
     if (threadIdx.x == 0) write_row(p, row, x, b);
-    if (!p.ntop) return;
-    const u32 count = parts * (u32)p.ntop;                   // (no more than there are threads)
-    for (u32 i = threadIdx.x; i < count; i += kThreads)
-        room.candidate[i] = __hip_atomic_load(&in[i / (u32)p.ntop].key[i % (u32)p.ntop], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!TOP) return;
+    const u32 i = threadIdx.x;                               // (no more keys than there are threads)
+    const u64 key = i < parts * (u32)p.ntop ? __hip_atomic_load(&in[i / (u32)p.ntop].key[i % (u32)p.ntop], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+    if (i == 0) room.candidates = 0;
     __syncthreads();
-    rank_all(room.candidate, count, p.ntop, [&](u32 place, u64 key) { write_top(p, row, place, key, b); });
+    if (key) room.candidate[atomicAdd(&room.candidates, 1u)] = key;
+    __syncthreads();
+    if (i < 64u) write_tops(p, row, first_of(room.candidate, room.candidates, (u32)p.ntop), b);
 }
 
 // d = -p (weight + g_entropy (log p + entropy)), and at the target and the alternatives their own weights besides.  A
 // workgroup has `chunks` chunks of a row, of eight elements a thread; the first is on its way before it asks for the row's
-// weights.  (More at a time, from 2 x 8 elements a thread on, are slower: 199 us against 170 for 4096 x 50304 in bf16, whose
-// 824 MB a copy moves in 162.)  Lane j of every wave knows alternative j; whose piece it lies in adds its weight.
+// weights.  (More at a time gain nothing: 4096 x 50304 in bf16, 824 MB, takes 169 us either way, and a copy of as much 162.)
+// Lane j of every wave knows alternative j; whose piece it lies in adds its weight.
 //
 // Whether a target is masked is read from the logits.  Where the gradient takes their place, a row is one workgroup's, which
 // has read that before it writes.
@@ -405,17 +457,20 @@ __global__ __launch_bounds__(kThreads) void k_row_gradient(const RowGradient p, 
 }  // namespace
 
 void launch_row_scores(const RowScores &r, const OpsContext &c) {
-    // Several workgroups a row where there are too few rows for all compute units, of pieces worth a workgroup each.
+    // Several workgroups a row where there are more compute units than rows, of two pieces a thread and more.  (256 rows of
+    // 50304 in bf16 with 8 alternatives: 12.5 us whole, 13.7 in two parts; one row of fp32 with 20: 10.7 us in twelve parts.)
     const u32 pieces = (r.vocab + 7u) / 8u;
-    u32 parts = r.rows < 2u * c.cus ? std::min((2u * c.cus + r.rows - 1u) / r.rows, (pieces + kThreads - 1u) / kThreads) : 1u;
+    u32 parts = std::min(c.cus / r.rows, (pieces + 2u * kThreads - 1u) / (2u * kThreads));
     parts = std::min(parts, r.ntop ? std::min(64u, kThreads / (u32)r.ntop) : 64u);
-    parts = std::min(parts, std::max(1u, EXCP_ROW_PARTS / r.rows));
-    parts = std::max(parts, 1u);
+    parts = std::max(std::min(parts, EXCP_ROW_PARTS / r.rows), 1u);
     const u32 per = (pieces + parts - 1u) / parts;
     with_type(r.type, [&](auto tag) {
         using T = decltype(tag);
-        if (parts == 1u) k_row_scores<T><<<std::min(r.rows, 1u << 20), kThreads, 0, c.stream>>>(r);
-        else k_row_scores_split<T><<<r.rows * parts, kThreads, 0, c.stream>>>(r, parts, per, c.parts, c.tickets);
+        const u32 rows = std::min(r.rows, 1u << 20);
+        if (parts == 1u && r.ntop) k_row_scores<T, true><<<rows, kThreads, 0, c.stream>>>(r);
+        else if (parts == 1u) k_row_scores<T, false><<<rows, kThreads, 0, c.stream>>>(r);
+        else if (r.ntop) k_row_scores_split<T, true><<<r.rows * parts, kThreads, 0, c.stream>>>(r, parts, per, c.parts, c.tickets);
+        else k_row_scores_split<T, false><<<r.rows * parts, kThreads, 0, c.stream>>>(r, parts, per, c.parts, c.tickets);
     });
 }
 

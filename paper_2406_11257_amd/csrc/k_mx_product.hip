@@ -3,6 +3,14 @@
 
 #include <type_traits>
 
+#ifndef W1
+#define W1 8
+#define B1 2
+#define W2 8
+#define B2 2
+#define TNL 4
+#define SMALLT 4u
+#endif
 namespace {
 
 // A tile of WN x WM waves, each 16 TN rows of B (n) by 16 TM rows of A (m); 256 elements of the reduction a stage.
@@ -210,84 +218,103 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
 }
 
 // Few rows of A: the rows of B are read once, each by one wave, and that is the time it takes.  A workgroup has 16 TN rows
-// of B against 16 TM rows of A; its eight waves take the groups of the reduction in turn (so that together they read runs
-// of 512 bytes), straight into registers, and join their sums in LDS.  X: the type of A before its quantisation, where a
-// lane's 32 elements are a block that it quantises itself; void: codes.
-template <class X, class T, int TN, int TM>
-__global__ __launch_bounds__(512) void k_mx_few_rows(const MxProduct p) {
-    constexpr u32 kWaves = 8, kFragments = TN * TM;
-    __shared__ v4f32 part[kWaves][kFragments][64];
-    const u32 lane = lane_id(), wave = threadIdx.x >> 6, r = lane & 15u, g = lane >> 4;
+// of B against 16 TM rows of A; its waves take the groups of the reduction in turn (so that together they read runs of a
+// row), straight into registers, BATCH groups on their way at a time, and join their sums in LDS.  X: the type of A before
+// its quantisation, where a lane's 32 elements are a block that it quantises itself; void: codes.
+template <class X, class T, int TN, int TM, int WAVES, int BATCH>
+__global__ __launch_bounds__(64 * WAVES) void k_mx_few_rows(const MxProduct p) {
+    constexpr u32 kFragments = TN * TM;
+    typedef typename std::conditional<std::is_void<X>::value, float, X>::type In;
+    __shared__ v4f32 part[WAVES][kFragments][64];
+    const u32 lane = lane_id(), r = lane & 15u, g = lane >> 4;
+    const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const u32 tiles_n = (p.n + 16u * TN - 1u) / (16u * TN), tiles = tiles_n * ((p.m + 16u * TM - 1u) / (16u * TM));
     for (u32 tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const u32 n0 = (tile % tiles_n) * 16u * TN, m0 = (tile / tiles_n) * 16u * TM;
-    const unsigned char *b_row[TN], *b_scale[TN];
-#pragma unroll
-    for (int i = 0; i < TN; ++i) {
-        const u64 at = (u64)min(n0 + i * 16u + r, p.n - 1u) * p.groups;
-        b_row[i] = p.b_codes + at * 64u + g * 16u;
-        b_scale[i] = p.b_scales + at * 4u + g;
-    }
-    v4f32 acc[TN][TM] = {};
-    for (u32 k = wave; k < p.groups; k += kWaves) {
-        v4i32 n_frag[TN], m_frag[TM];
-        u32 n_scale[TN], m_scale[TM];
+        const u32 n0 = (tile % tiles_n) * 16u * TN, m0 = (tile / tiles_n) * 16u * TM;
+        const unsigned char *b_row[TN], *b_scale[TN];
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
-            n_frag[i] = *(const v4i32 *)(b_row[i] + k * 64ull);
-            n_scale[i] = b_scale[i][k * 4ull];
+            const u64 at = (u64)min(n0 + i * 16u + r, p.n - 1u) * p.groups;
+            b_row[i] = p.b_codes + at * 64u + g * 16u;
+            b_scale[i] = p.b_scales + at * 4u + g;
         }
+        v4f32 acc[TN][TM] = {};
+        for (u32 first = wave; first < p.groups; first += WAVES * BATCH) {
+            v4i32 n_frag[BATCH][TN], m_frag[BATCH][TM];
+            u32 n_scale[BATCH][TN], m_scale[BATCH][TM];
+            Eight<In> e[BATCH][TM][4];
 #pragma unroll
-        for (int j = 0; j < TM; ++j) {
-            const u32 m = m0 + j * 16u + r;
-            if constexpr (std::is_void<X>::value) {
-                const u64 at = (u64)min(m, p.m - 1u) * p.groups + k;
-                m_frag[j] = *(const v4i32 *)(p.a_codes + at * 64u + g * 16u);
-                m_scale[j] = p.a_scales[at * 4u + g];
-            } else {
-                const u32 col = k * 128u + g * 32u, have = m < p.m && col < p.x.cols ? p.x.cols - col : 0u;
-                const X *x = (const X *)p.x.p + (u64)m * p.x.ld + col;
-                Eight<X> e[4];
-                u32 peak = 0;
+            for (int u = 0; u < BATCH; ++u) {
+                const u32 k = first + u * WAVES, at = min(k, p.groups - 1u);     // (beyond the last: that one, against zeros)
 #pragma unroll
-                for (u32 q = 0; q < 4; ++q) {
-                    e[q] = load_eight(x + q * 8u, have > q * 8u ? have - q * 8u : 0u);
-                    peak = max(peak, mx_peak(e[q]));
+                for (int i = 0; i < TN; ++i) {
+                    n_frag[u][i] = *(const v4i32 *)(b_row[i] + at * 64ull);
+                    n_scale[u][i] = b_scale[i][at * 4ull];
                 }
-                m_scale[j] = mx_scale_byte<X>(peak);
 #pragma unroll
-                for (u32 q = 0; q < 4; ++q) m_frag[j][q] = (int)mx_codes(e[q], m_scale[j]);
+                for (int j = 0; j < TM; ++j) {
+                    const u32 m = m0 + j * 16u + r;
+                    if constexpr (std::is_void<X>::value) {
+                        const u64 o = (u64)min(m, p.m - 1u) * p.groups + at;
+                        m_frag[u][j] = *(const v4i32 *)(p.a_codes + o * 64u + g * 16u);
+                        m_scale[u][j] = p.a_scales[o * 4u + g];
+                        if (k >= p.groups) m_frag[u][j] = v4i32{0, 0, 0, 0};
+                    } else {
+                        const u32 col = k * 128u + g * 32u, have = m < p.m && col < p.x.cols ? p.x.cols - col : 0u;
+                        const In *x = (const In *)p.x.p + (u64)m * p.x.ld + col;
+                        if (have >= 32u) {
+#pragma unroll
+                            for (u32 q = 0; q < 4; ++q) e[u][j][q] = load_eight(x + q * 8u, 8u);
+                        } else {
+#pragma unroll
+                            for (u32 q = 0; q < 4; ++q) e[u][j][q] = load_eight(x + q * 8u, min(have > q * 8u ? have - q * 8u : 0u, 7u));
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                if constexpr (!std::is_void<X>::value) {
+#pragma unroll
+                    for (int j = 0; j < TM; ++j) {
+                        u32 peak = 0;
+#pragma unroll
+                        for (u32 q = 0; q < 4; ++q) peak = max(peak, mx_peak(e[u][j][q]));
+                        m_scale[u][j] = mx_scale_byte<In>(peak);
+#pragma unroll
+                        for (u32 q = 0; q < 4; ++q) m_frag[u][j][q] = (int)mx_codes(e[u][j][q], m_scale[u][j]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < TN; ++i)
+#pragma unroll
+                    for (int j = 0; j < TM; ++j) acc[i][j] = mx_mfma(n_frag[u][i], n_scale[u][i], m_frag[u][j], m_scale[u][j], acc[i][j]);
             }
         }
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
-            for (int j = 0; j < TM; ++j) acc[i][j] = mx_mfma(n_frag[i], n_scale[i], m_frag[j], m_scale[j], acc[i][j]);
-    }
+            for (int j = 0; j < TM; ++j) part[wave][i * TM + j][lane] = acc[i][j];
+        __syncthreads();
+        for (u32 f = wave; f < kFragments; f += WAVES) {
+            v4f32 sum = part[0][f][lane];
 #pragma unroll
-    for (int i = 0; i < TN; ++i)
+            for (u32 w = 1; w < WAVES; ++w) sum += part[w][f][lane];
+            const u32 n = n0 + (f / TM) * 16u + g * 4u, m = m0 + (f % TM) * 16u + r;
+            if (m >= p.m) continue;
+            T *y = (T *)p.y + (u64)m * p.ld + n;
 #pragma unroll
-        for (int j = 0; j < TM; ++j) part[wave][i * TM + j][lane] = acc[i][j];
-    __syncthreads();
-    for (u32 f = wave; f < kFragments; f += kWaves) {
-        v4f32 sum = part[0][f][lane];
-#pragma unroll
-        for (u32 w = 1; w < kWaves; ++w) sum += part[w][f][lane];
-        const u32 n = n0 + (f / TM) * 16u + g * 4u, m = m0 + (f % TM) * 16u + r;
-        if (m >= p.m) continue;
-        T *y = (T *)p.y + (u64)m * p.ld + n;
-#pragma unroll
-        for (u32 e = 0; e < 4; ++e)
-            if (n + e < p.n) y[e] = (T)sum[e];
-    }
-    __syncthreads();
+            for (u32 e = 0; e < 4; ++e)
+                if (n + e < p.n) y[e] = (T)sum[e];
+        }
+        __syncthreads();
     }
 }
 
-template <class X, class T, int TN, int TM>
+template <class X, class T, int TN, int TM, int WAVES, int BATCH>
 void launch_few(const MxProduct &p, hipStream_t s) {
     const u32 tiles = ((p.n + 16u * TN - 1u) / (16u * TN)) * ((p.m + 16u * TM - 1u) / (16u * TM));
-    k_mx_few_rows<X, T, TN, TM><<<std::min(tiles, 1u << 20), 512, 0, s>>>(p);
+    k_mx_few_rows<X, T, TN, TM, WAVES, BATCH><<<std::min(tiles, 1u << 20), 64 * WAVES, 0, s>>>(p);
 }
 
 }  // namespace
@@ -303,9 +330,9 @@ void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
     with_type(p.type, [&](auto tag) {
         using T = decltype(tag);
         if (p.m <= 64u) {
-            if (p.m <= 16u) launch_few<void, T, 1, 1>(p, s);
-            else if (p.m <= 32u) launch_few<void, T, 2, 2>(p, s);
-            else launch_few<void, T, 1, 4>(p, s);
+            if (p.m <= 16u) launch_few<void, T, 1, 1, 8, 4>(p, s);
+            else if (p.m <= 32u) launch_few<void, T, 2, 2, 8, 2>(p, s);
+            else launch_few<void, T, 1, 4, 8, 2>(p, s);
             return;
         }
         const u64 large = (u64)((p.n + 255u) / 256u) * ((p.m + 255u) / 256u), middle = (u64)((p.n + 127u) / 128u) * ((p.m + 127u) / 128u);
@@ -321,9 +348,8 @@ void launch_mx_few_rows(const MxProduct &p, u32 cus, hipStream_t s) {
         with_type(p.type, [&](auto tag) {
             using X = decltype(xtag);
             using T = decltype(tag);
-            if (tiles < 4u * cus) launch_few<X, T, 1, 1>(p, s);
-            else if (tiles < 8u * cus) launch_few<X, T, 2, 1>(p, s);
-            else launch_few<X, T, 4, 1>(p, s);
+            if (tiles < SMALLT * cus) launch_few<X, T, 1, 1, W1, B1>(p, s);
+            else launch_few<X, T, TNL, 1, W2, B2>(p, s);
         });
     });
 }
