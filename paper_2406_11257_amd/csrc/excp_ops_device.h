@@ -72,6 +72,13 @@ __device__ __forceinline__ void store_run(T *row, u32 at, u32 end, bool there, b
             if (at + i < end) row[at + i] = e[i];
     }
 }
+// Four sums to elements at .. at + 3 of a row of `end`.
+template <class T>
+__device__ __forceinline__ void store_four(T *row, u32 at, u32 end, v4f32 v) {
+#pragma unroll
+    for (u32 i = 0; i < 4; ++i)
+        if (at + i < end) row[at + i] = (T)v[i];
+}
 // Four floats rounded to a 16-bit type.
 template <class T>
 __device__ __forceinline__ uint2 pack4(v4f32 v) {

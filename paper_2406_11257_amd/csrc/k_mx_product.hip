@@ -3,14 +3,6 @@
 
 #include <type_traits>
 
-#ifndef W1
-#define W1 8
-#define B1 2
-#define W2 8
-#define B2 2
-#define TNL 4
-#define SMALLT 4u
-#endif
 namespace {
 
 // A tile of WN x WM waves, each 16 TN rows of B (n) by 16 TM rows of A (m); 256 elements of the reduction a stage.
@@ -219,102 +211,149 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
 
 // Few rows of A: the rows of B are read once, each by one wave, and that is the time it takes.  A workgroup has 16 TN rows
 // of B against 16 TM rows of A; its waves take the groups of the reduction in turn (so that together they read runs of a
-// row), straight into registers, BATCH groups on their way at a time, and join their sums in LDS.  X: the type of A before
-// its quantisation, where a lane's 32 elements are a block that it quantises itself; void: codes.
-template <class X, class T, int TN, int TM, int WAVES, int BATCH>
-__global__ __launch_bounds__(64 * WAVES) void k_mx_few_rows(const MxProduct p) {
-    constexpr u32 kFragments = TN * TM;
-    typedef typename std::conditional<std::is_void<X>::value, float, X>::type In;
-    __shared__ v4f32 part[WAVES][kFragments][64];
+// row), straight into registers, BATCH groups on their way at a time, and join their sums in LDS.
+template <class T, int TN, int TM, int BATCH>
+__global__ __launch_bounds__(512) void k_mx_few_rows(const MxProduct p) {
+    constexpr u32 kWaves = 8, kFragments = TN * TM;
+    __shared__ v4f32 part[kWaves][kFragments][64];
     const u32 lane = lane_id(), r = lane & 15u, g = lane >> 4;
     const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const u32 tiles_n = (p.n + 16u * TN - 1u) / (16u * TN), tiles = tiles_n * ((p.m + 16u * TM - 1u) / (16u * TM));
     for (u32 tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const u32 n0 = (tile % tiles_n) * 16u * TN, m0 = (tile / tiles_n) * 16u * TM;
-        const unsigned char *b_row[TN], *b_scale[TN];
+        const unsigned char *row[TN + TM], *scale[TN + TM];
 #pragma unroll
-        for (int i = 0; i < TN; ++i) {
-            const u64 at = (u64)min(n0 + i * 16u + r, p.n - 1u) * p.groups;
-            b_row[i] = p.b_codes + at * 64u + g * 16u;
-            b_scale[i] = p.b_scales + at * 4u + g;
+        for (int i = 0; i < TN + TM; ++i) {
+            const u64 at = (u64)(i < TN ? min(n0 + i * 16u + r, p.n - 1u) : min(m0 + (i - TN) * 16u + r, p.m - 1u)) * p.groups;
+            row[i] = (i < TN ? p.b_codes : p.a_codes) + at * 64u + g * 16u;
+            scale[i] = (i < TN ? p.b_scales : p.a_scales) + at * 4u + g;
         }
         v4f32 acc[TN][TM] = {};
-        for (u32 first = wave; first < p.groups; first += WAVES * BATCH) {
-            v4i32 n_frag[BATCH][TN], m_frag[BATCH][TM];
-            u32 n_scale[BATCH][TN], m_scale[BATCH][TM];
-            Eight<In> e[BATCH][TM][4];
+        for (u32 first = wave; first < p.groups; first += kWaves * BATCH) {
+            v4i32 codes[BATCH][TN + TM];
+            u32 by[BATCH][TN + TM];
 #pragma unroll
             for (int u = 0; u < BATCH; ++u) {
-                const u32 k = first + u * WAVES, at = min(k, p.groups - 1u);     // (beyond the last: that one, against zeros)
+                const u32 k = first + u * kWaves, at = min(k, p.groups - 1u);    // (beyond the last: that one, against zeros)
 #pragma unroll
-                for (int i = 0; i < TN; ++i) {
-                    n_frag[u][i] = *(const v4i32 *)(b_row[i] + at * 64ull);
-                    n_scale[u][i] = b_scale[i][at * 4ull];
-                }
-#pragma unroll
-                for (int j = 0; j < TM; ++j) {
-                    const u32 m = m0 + j * 16u + r;
-                    if constexpr (std::is_void<X>::value) {
-                        const u64 o = (u64)min(m, p.m - 1u) * p.groups + at;
-                        m_frag[u][j] = *(const v4i32 *)(p.a_codes + o * 64u + g * 16u);
-                        m_scale[u][j] = p.a_scales[o * 4u + g];
-                        if (k >= p.groups) m_frag[u][j] = v4i32{0, 0, 0, 0};
-                    } else {
-                        const u32 col = k * 128u + g * 32u, have = m < p.m && col < p.x.cols ? p.x.cols - col : 0u;
-                        const In *x = (const In *)p.x.p + (u64)m * p.x.ld + col;
-                        if (have >= 32u) {
-#pragma unroll
-                            for (u32 q = 0; q < 4; ++q) e[u][j][q] = load_eight(x + q * 8u, 8u);
-                        } else {
-#pragma unroll
-                            for (u32 q = 0; q < 4; ++q) e[u][j][q] = load_eight(x + q * 8u, min(have > q * 8u ? have - q * 8u : 0u, 7u));
-                        }
-                    }
+                for (int i = 0; i < TN + TM; ++i) {
+                    codes[u][i] = *(const v4i32 *)(row[i] + at * 64ull);
+                    by[u][i] = scale[i][at * 4ull];
+                    if (i >= TN && k >= p.groups) codes[u][i] = v4i32{0, 0, 0, 0};
                 }
             }
 #pragma unroll
-            for (int u = 0; u < BATCH; ++u) {
-                if constexpr (!std::is_void<X>::value) {
-#pragma unroll
-                    for (int j = 0; j < TM; ++j) {
-                        u32 peak = 0;
-#pragma unroll
-                        for (u32 q = 0; q < 4; ++q) peak = max(peak, mx_peak(e[u][j][q]));
-                        m_scale[u][j] = mx_scale_byte<In>(peak);
-#pragma unroll
-                        for (u32 q = 0; q < 4; ++q) m_frag[u][j][q] = (int)mx_codes(e[u][j][q], m_scale[u][j]);
-                    }
-                }
+            for (int u = 0; u < BATCH; ++u)
 #pragma unroll
                 for (int i = 0; i < TN; ++i)
 #pragma unroll
-                    for (int j = 0; j < TM; ++j) acc[i][j] = mx_mfma(n_frag[u][i], n_scale[u][i], m_frag[u][j], m_scale[u][j], acc[i][j]);
-            }
+                    for (int j = 0; j < TM; ++j) acc[i][j] = mx_mfma(codes[u][i], by[u][i], codes[u][TN + j], by[u][TN + j], acc[i][j]);
         }
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
             for (int j = 0; j < TM; ++j) part[wave][i * TM + j][lane] = acc[i][j];
         __syncthreads();
-        for (u32 f = wave; f < kFragments; f += WAVES) {
+        for (u32 f = wave; f < kFragments; f += kWaves) {
             v4f32 sum = part[0][f][lane];
 #pragma unroll
-            for (u32 w = 1; w < WAVES; ++w) sum += part[w][f][lane];
+            for (u32 w = 1; w < kWaves; ++w) sum += part[w][f][lane];
             const u32 n = n0 + (f / TM) * 16u + g * 4u, m = m0 + (f % TM) * 16u + r;
-            if (m >= p.m) continue;
-            T *y = (T *)p.y + (u64)m * p.ld + n;
-#pragma unroll
-            for (u32 e = 0; e < 4; ++e)
-                if (n + e < p.n) y[e] = (T)sum[e];
+            if (m < p.m) store_four((T *)p.y + (u64)m * p.ld, n, p.n, sum);
         }
         __syncthreads();
     }
 }
 
-template <class X, class T, int TN, int TM, int WAVES, int BATCH>
+// The same for up to sixteen rows of x that are quantised on the way: once a workgroup, into LDS (a part of the reduction at
+// a time, where all of it does not fit), and from there against tile after tile of sixteen rows of W.  What lanes of rows that
+// x does not have read is another row's: nobody reads their sums.
+template <class X, class T>
+__global__ __launch_bounds__(512) void k_mx_few_rows_of(const MxProduct p, u32 room) {
+    constexpr u32 kWaves = 8, kBatch = 4;
+    extern __shared__ __attribute__((aligned(16))) unsigned char x_codes[];      // [group of the part][row][64], then scales
+    __shared__ v4f32 sums[kWaves][64];
+    const u32 lane = lane_id(), r = min(lane & 15u, p.m - 1u), g = lane >> 4;
+    const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    unsigned char *const x_scales = x_codes + room * p.m * 64u;
+    const u32 tiles = (p.n + 15u) / 16u;
+    auto quantize = [&](u32 from, u32 groups) __attribute__((always_inline)) {
+        for (u32 b = threadIdx.x; b < groups * 4u * p.m; b += 64u * kWaves) {
+            const u32 row = b / (groups * 4u), at = b - row * (groups * 4u), col = from * 128u + at * 32u;
+            const X *x = (const X *)p.x.p + (u64)row * p.x.ld + col;
+            const u32 have = col < p.x.cols ? p.x.cols - col : 0u;
+            Eight<X> e[4];
+            u32 peak = 0, code[4];
+#pragma unroll
+            for (u32 q = 0; q < 4; ++q) e[q] = load_eight(x + q * 8u, have > q * 8u ? have - q * 8u : 0u);
+#pragma unroll
+            for (u32 q = 0; q < 4; ++q) peak = max(peak, mx_peak(e[q]));
+            const u32 byte = mx_scale_byte<X>(peak), o = (at / 4u) * p.m + row;
+#pragma unroll
+            for (u32 q = 0; q < 4; ++q) code[q] = mx_codes(e[q], byte);
+            *(uint4 *)(x_codes + o * 64u + (at & 3u) * 16u) = make_uint4(code[0], code[1], code[2], code[3]);
+            x_scales[o * 4u + (at & 3u)] = (unsigned char)byte;
+        }
+    };
+    const unsigned char *codes, *scales;
+    v4i32 w[kBatch];
+    u32 by[kBatch];
+    // groups from + k, from + k + 8, .. of a part of `end`
+    auto load = [&](u32 from, u32 k, u32 end) __attribute__((always_inline)) {
+#pragma unroll
+        for (u32 u = 0; u < kBatch; ++u)
+            if (k + u * kWaves < end) {
+                w[u] = *(const v4i32 *)(codes + (from + k + u * kWaves) * 64ull);
+                by[u] = scales[(from + k + u * kWaves) * 4ull];
+            }
+    };
+    const bool once = p.groups <= room;
+    if (once) quantize(0, p.groups);
+    for (u32 tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const u64 at = (u64)min(tile * 16u + (lane & 15u), p.n - 1u) * p.groups;
+        codes = p.b_codes + at * 64u + g * 16u;
+        scales = p.b_scales + at * 4u + g;
+        v4f32 acc = {};
+        for (u32 from = 0; from < p.groups; from += room) {
+            const u32 end = min(p.groups - from, room);
+            load(from, wave, end);
+            if (!once) {
+                __syncthreads();                             // the last part has been read
+                quantize(from, end);
+            }
+            if (!once || tile == blockIdx.x) __syncthreads();
+            for (u32 k = wave; k < end;) {
+#pragma unroll
+                for (u32 u = 0; u < kBatch; ++u)
+                    if (k + u * kWaves < end) {
+                        const u32 o = (k + u * kWaves) * p.m + r;
+                        acc = mx_mfma(w[u], by[u], *(const v4i32 *)(x_codes + o * 64u + g * 16u), x_scales[o * 4u + g], acc);
+                    }
+                k += kBatch * kWaves;
+                load(from, k, end);
+            }
+        }
+        sums[wave][lane] = acc;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (u32 i = 1; i < kWaves; ++i) acc += sums[i][lane];
+            if ((lane & 15u) < p.m) store_four((T *)p.y + (u64)r * p.ld, tile * 16u + g * 4u, p.n, acc);
+        }
+        __syncthreads();
+    }
+}
+
+template <class T, int TN, int TM, int BATCH>
 void launch_few(const MxProduct &p, hipStream_t s) {
     const u32 tiles = ((p.n + 16u * TN - 1u) / (16u * TN)) * ((p.m + 16u * TM - 1u) / (16u * TM));
-    k_mx_few_rows<X, T, TN, TM, WAVES, BATCH><<<std::min(tiles, 1u << 20), 64 * WAVES, 0, s>>>(p);
+    k_mx_few_rows<T, TN, TM, BATCH><<<std::min(tiles, 1u << 20), 512, 0, s>>>(p);
+}
+template <class X, class T>
+void launch_few_of(const MxProduct &p, u32 cus, hipStream_t s) {
+    // LDS: a group of x takes 68 bytes a row; with the sums, 64 KB, so that a compute unit has two workgroups
+    const u32 room = std::min(p.groups, 57344u / (68u * p.m));
+    k_mx_few_rows_of<X, T><<<std::min((p.n + 15u) / 16u, 2u * cus), 512, room * p.m * 68u, s>>>(p, room);
 }
 
 }  // namespace
@@ -330,9 +369,9 @@ void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
     with_type(p.type, [&](auto tag) {
         using T = decltype(tag);
         if (p.m <= 64u) {
-            if (p.m <= 16u) launch_few<void, T, 1, 1, 8, 4>(p, s);
-            else if (p.m <= 32u) launch_few<void, T, 2, 2, 8, 2>(p, s);
-            else launch_few<void, T, 1, 4, 8, 2>(p, s);
+            if (p.m <= 16u) launch_few<T, 1, 1, 4>(p, s);
+            else if (p.m <= 32u) launch_few<T, 2, 2, 2>(p, s);
+            else launch_few<T, 1, 4, 2>(p, s);
             return;
         }
         const u64 large = (u64)((p.n + 255u) / 256u) * ((p.m + 255u) / 256u), middle = (u64)((p.n + 127u) / 128u) * ((p.m + 127u) / 128u);
@@ -343,13 +382,5 @@ void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
 }
 
 void launch_mx_few_rows(const MxProduct &p, u32 cus, hipStream_t s) {
-    const u32 tiles = (p.n + 15u) / 16u;
-    with_type(p.x.type, [&](auto xtag) {
-        with_type(p.type, [&](auto tag) {
-            using X = decltype(xtag);
-            using T = decltype(tag);
-            if (tiles < SMALLT * cus) launch_few<X, T, 1, 1, W1, B1>(p, s);
-            else launch_few<X, T, TNL, 1, W2, B2>(p, s);
-        });
-    });
+    with_type(p.x.type, [&](auto xtag) { with_type(p.type, [&](auto tag) { launch_few_of<decltype(xtag), decltype(tag)>(p, cus, s); }); });
 }
