@@ -222,33 +222,35 @@ def _load_types():
     _types.update({torch.float32: EXCP_TYPE_F32, torch.float16: EXCP_TYPE_F16, torch.bfloat16: EXCP_TYPE_BF16})
 
 
-def _type_of(t, name, device):
-    """EXCP_TYPE_* of a matrix on the context's device whose rows are contiguous."""
+def _matrix(t, name, gpu):
+    """(address, EXCP_TYPE_*, rows, columns, ld) of a matrix on that GPU whose rows are contiguous."""
     kind = _types.get(t.dtype)
-    if kind is None or t.dim() != 2 or t.device != device or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise TypeError(f"{name} must be a float32, float16 or bfloat16 matrix on {device} with contiguous rows")
-    return kind
+    if kind is not None and t.get_device() == gpu and t.dim() == 2:
+        rows, cols = t.shape
+        ld, step = t.stride()
+        if step == 1 or cols <= 1:
+            return t.data_ptr(), kind, rows, cols, ld if rows > 1 else cols
+    raise TypeError(f"{name} must be a float32, float16 or bfloat16 matrix on cuda:{gpu} with contiguous rows")
 
 
-def _ld(t, rows, cols):
-    return t.stride(0) if rows > 1 else cols
-
-
-def _check_vec(t, name, dtype, shape, device):
-    if t is None or t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise TypeError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device}")
+def _vector(t, name, dtype, shape, gpu):
+    """Address of a contiguous tensor of that type and shape, or None for none."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != gpu or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on cuda:{gpu}")
     return t.data_ptr()
 
 
-def _opt_vec(t, name, dtype, shape, device):
-    return None if t is None else _check_vec(t, name, dtype, shape, device)
-
-
-def _check_coded(codes, scales, rows, cols, name, device):
-    """Codes and scales of a rows x cols matrix, as mx_empty makes them."""
-    groups = (cols + 127) // 128
-    return (_check_vec(codes, name + " codes", _uint8, (rows, groups * 64), device),
-            _check_vec(scales, name + " scales", _uint8, (rows, groups * 4), device))
+def _coded(codes, scales, rows, cols, name, gpu):
+    """Addresses of the codes and scales of a rows x cols matrix, as mx_empty makes them."""
+    groups = (cols + 127) >> 7
+    if (codes is None or scales is None or codes.dtype is not _uint8 or scales.dtype is not _uint8
+            or codes.shape != (rows, groups * 64) or scales.shape != (rows, groups * 4)
+            or not codes.is_contiguous() or not scales.is_contiguous() or codes.get_device() != gpu or scales.get_device() != gpu):
+        raise TypeError(f"{name} codes and scales must be contiguous uint8 tensors of shapes {(rows, groups * 64)} and "
+                        f"{(rows, groups * 4)} on cuda:{gpu}")
+    return codes.data_ptr(), scales.data_ptr()
 
 
 def mx_empty(rows: int, cols: int, device="cuda"):
@@ -495,40 +497,49 @@ class Context:
     def excp_mx_quantize(self, x, codes=None, scales=None, codes_t=None, scales_t=None):
         """x (a matrix) into codes and scales of its rows, and (or) of its columns: tensors as mx_empty makes them for
         x's shape and for its transpose's."""
-        device, kind, (rows, cols) = self.device, _type_of(x, "x", self.device), x.shape
-        c, s = (None, None) if codes is None else _check_coded(codes, scales, rows, cols, "the rows'", device)
-        ct, st = (None, None) if codes_t is None else _check_coded(codes_t, scales_t, cols, rows, "the columns'", device)
-        rc = lib().excp_mx_quantize(self._h, x.data_ptr(), kind, rows, cols, _ld(x, rows, cols), c, s, ct, st)
+        gpu = self.device.index
+        ptr, kind, rows, cols, ld = _matrix(x, "x", gpu)
+        c = s = ct = st = None
+        if codes is not None:
+            c, s = _coded(codes, scales, rows, cols, "the rows'", gpu)
+        if codes_t is not None:
+            ct, st = _coded(codes_t, scales_t, cols, rows, "the columns'", gpu)
+        rc = lib().excp_mx_quantize(self._h, ptr, kind, rows, cols, ld, c, s, ct, st)
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_mx_quantize")
 
     def excp_mx_dequantize(self, codes, scales, x):
         """The values of codes and scales into the matrix x."""
-        kind, (rows, cols) = _type_of(x, "x", self.device), x.shape
-        c, s = _check_coded(codes, scales, rows, cols, "x's", self.device)
-        rc = lib().excp_mx_dequantize(self._h, c, s, rows, cols, x.data_ptr(), kind, _ld(x, rows, cols))
+        gpu = self.device.index
+        ptr, kind, rows, cols, ld = _matrix(x, "x", gpu)
+        c, s = _coded(codes, scales, rows, cols, "x's", gpu)
+        rc = lib().excp_mx_dequantize(self._h, c, s, rows, cols, ptr, kind, ld)
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_mx_dequantize")
 
     def excp_mx_matmul(self, a_codes, a_scales, b_codes, b_scales, k, y):
         """y (m x n) = A B^T of A (m x k) and B (n x k) in codes and scales."""
-        device, kind, (m, n) = self.device, _type_of(y, "y", self.device), y.shape
-        a, sa = _check_coded(a_codes, a_scales, m, k, "A's", device)
-        b, sb = _check_coded(b_codes, b_scales, n, k, "B's", device)
-        rc = lib().excp_mx_matmul(self._h, a, sa, b, sb, m, n, k, y.data_ptr(), kind, _ld(y, m, n))
+        gpu = self.device.index
+        ptr, kind, m, n, ld = _matrix(y, "y", gpu)
+        a, sa = _coded(a_codes, a_scales, m, k, "A's", gpu)
+        b, sb = _coded(b_codes, b_scales, n, k, "B's", gpu)
+        rc = lib().excp_mx_matmul(self._h, a, sa, b, sb, m, n, k, ptr, kind, ld)
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_mx_matmul")
 
     def excp_mx_linear(self, x, w_codes, w_scales, y, x_codes=None, x_scales=None):
         """y (m x n) = MX(x) W^T; x_codes and x_scales (as mx_empty makes them for x) are room to work in, not needed
         for up to EXCP_MX_FEW_ROWS rows."""
-        device, kind, (m, k) = self.device, _type_of(x, "x", self.device), x.shape
-        ykind, (my, n) = _type_of(y, "y", device), y.shape
+        gpu = self.device.index
+        xp, xkind, m, k, ldx = _matrix(x, "x", gpu)
+        yp, ykind, my, n, ldy = _matrix(y, "y", gpu)
         if my != m:
             raise ValueError("x and y differ in rows")
-        w, sw = _check_coded(w_codes, w_scales, n, k, "W's", device)
-        c, s = (None, None) if x_codes is None else _check_coded(x_codes, x_scales, m, k, "x's", device)
-        rc = lib().excp_mx_linear(self._h, x.data_ptr(), kind, _ld(x, m, k), w, sw, m, n, k, y.data_ptr(), ykind, _ld(y, m, n), c, s)
+        w, sw = _coded(w_codes, w_scales, n, k, "W's", gpu)
+        c = s = None
+        if x_codes is not None:
+            c, s = _coded(x_codes, x_scales, m, k, "x's", gpu)
+        rc = lib().excp_mx_linear(self._h, xp, xkind, ldx, w, sw, m, n, k, yp, ykind, ldy, c, s)
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_mx_linear")
 
@@ -537,35 +548,36 @@ class Context:
         """Statistics of every row of logits into the tensors given: logprob of the row's target and entropy (float32,
         one a row), lse in two parts to be added (float32, rows x 2), the largest log probabilities and their indices
         (float32 and int64, rows x ntop)."""
-        device, kind, (rows, vocab) = self.device, _type_of(logits, "logits", self.device), logits.shape
+        gpu = self.device.index
+        ptr, kind, rows, vocab, ld = _matrix(logits, "logits", gpu)
         top = top_ids if top_logprob is None else top_logprob
         ntop = 0 if top is None else top.shape[-1]
-        rc = lib().excp_token_logprobs(self._h, logits.data_ptr(), kind, rows, vocab, _ld(logits, rows, vocab),
-                                       _opt_vec(targets, "targets", _int64, (rows,), device), ntop,
-                                       _opt_vec(logprob, "logprob", _float32, (rows,), device),
-                                       _opt_vec(entropy, "entropy", _float32, (rows,), device),
-                                       _opt_vec(lse, "lse", _float32, (rows, 2), device),
-                                       _opt_vec(top_logprob, "top_logprob", _float32, (rows, ntop), device),
-                                       _opt_vec(top_ids, "top_ids", _int64, (rows, ntop), device))
+        rc = lib().excp_token_logprobs(self._h, ptr, kind, rows, vocab, ld, _vector(targets, "targets", _int64, (rows,), gpu), ntop,
+                                       _vector(logprob, "logprob", _float32, (rows,), gpu),
+                                       _vector(entropy, "entropy", _float32, (rows,), gpu),
+                                       _vector(lse, "lse", _float32, (rows, 2), gpu),
+                                       _vector(top_logprob, "top_logprob", _float32, (rows, ntop), gpu),
+                                       _vector(top_ids, "top_ids", _int64, (rows, ntop), gpu))
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_token_logprobs")
 
     def excp_token_logprobs_backward(self, logits, targets, lse, entropy, top_ids, g_logprob, g_entropy, g_top, dlogits):
         """The gradient over the logits, into dlogits (which may be the logits), from what excp_token_logprobs wrote;
         each g may be None."""
-        device, kind, (rows, vocab) = self.device, _type_of(logits, "logits", self.device), logits.shape
-        if _type_of(dlogits, "dlogits", device) != kind or dlogits.shape != logits.shape:
+        gpu = self.device.index
+        ptr, kind, rows, vocab, ld = _matrix(logits, "logits", gpu)
+        dptr, dkind, drows, dvocab, ldd = _matrix(dlogits, "dlogits", gpu)
+        if dkind != kind or drows != rows or dvocab != vocab:
             raise TypeError("dlogits must have the logits' type and shape")
         ntop = 0 if g_top is None else g_top.shape[-1]
-        rc = lib().excp_token_logprobs_backward(self._h, logits.data_ptr(), kind, rows, vocab, _ld(logits, rows, vocab),
-                                                _opt_vec(targets, "targets", _int64, (rows,), device),
-                                                _opt_vec(lse, "lse", _float32, (rows, 2), device),
-                                                _opt_vec(entropy, "entropy", _float32, (rows,), device),
-                                                _opt_vec(top_ids, "top_ids", _int64, (rows, ntop), device) if ntop else None, ntop,
-                                                _opt_vec(g_logprob, "g_logprob", _float32, (rows,), device),
-                                                _opt_vec(g_entropy, "g_entropy", _float32, (rows,), device),
-                                                _opt_vec(g_top, "g_top", _float32, (rows, ntop), device),
-                                                dlogits.data_ptr(), _ld(dlogits, rows, vocab))
+        rc = lib().excp_token_logprobs_backward(self._h, ptr, kind, rows, vocab, ld,
+                                                _vector(targets, "targets", _int64, (rows,), gpu),
+                                                _vector(lse, "lse", _float32, (rows, 2), gpu),
+                                                _vector(entropy, "entropy", _float32, (rows,), gpu),
+                                                _vector(top_ids, "top_ids", _int64, (rows, ntop), gpu) if ntop else None, ntop,
+                                                _vector(g_logprob, "g_logprob", _float32, (rows,), gpu),
+                                                _vector(g_entropy, "g_entropy", _float32, (rows,), gpu),
+                                                _vector(g_top, "g_top", _float32, (rows, ntop), gpu), dptr, ldd)
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_token_logprobs_backward")
 

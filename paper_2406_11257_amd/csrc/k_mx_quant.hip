@@ -3,6 +3,8 @@
 // All three are bound by memory: 2 or 4 bytes an element one way, 0.53 the other.
 #include "excp_ops_device.h"
 
+#include <type_traits>
+
 namespace {
 
 constexpr u32 kThreads = 256;
@@ -57,21 +59,29 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize_tile(const T *__restri
                                                                unsigned char *__restrict__ codes_t, unsigned char *__restrict__ scales_t) {
     constexpr u32 kPitch = TileRoom<T>::pitch;
     __shared__ TileRoom<T> room;
-    const u32 tiles_r = (rows + 127u) / 128u;
+    const u32 tiles_r = (rows + 127u) / 128u, at = threadIdx.x & 15u, first = threadIdx.x / 16u;
     for (u64 tile = blockIdx.x; tile < (u64)tiles_r * tiles_c; tile += gridDim.x) {
-    const u32 tile_r = (u32)(tile / tiles_c), tile_c = (u32)(tile - (u64)tile_r * tiles_c);
-    const u32 at = threadIdx.x & 15u, col = tile_c * 128u + at * 8u;
+    const u32 tile_r = (u32)(tile / tiles_c), tile_c = (u32)(tile - (u64)tile_r * tiles_c), col = tile_c * 128u + at * 8u;
+    Eight<T> v[8];
 #pragma unroll
     for (u32 q = 0; q < 8; ++q) {
-        const u32 in = q * 16u + threadIdx.x / 16u, row = tile_r * 128u + in;
-        const Eight<T> v = load_eight(x + (u64)row * ld + col, row < rows && col < cols ? cols - col : 0u);
-        u32 w[8 * sizeof(T) / 4];
-        __builtin_memcpy(w, &v, sizeof w);
+        const u32 row = tile_r * 128u + q * 16u + first;
+        v[q] = load_eight(x + (u64)row * ld + col, row < rows && col < cols ? cols - col : 0u);
+    }
 #pragma unroll
-        for (u32 i = 0; i < 8 * sizeof(T) / 4; ++i) room.word[in * kPitch + at * (8 * sizeof(T) / 4) + i] = w[i];
-        if (codes) {                                         // the same for all
-            const u32 byte = mx_scale_byte<T>(quad_max(mx_peak(v)));
-            const u32 code = mx_codes(v, byte), four = group_scales(byte);
+    for (u32 q = 0; q < 8; ++q) {
+        u32 w[8 * sizeof(T) / 4];
+        __builtin_memcpy(w, &v[q], sizeof w);
+#pragma unroll
+        for (u32 i = 0; i < 8 * sizeof(T) / 4; ++i) room.word[(q * 16u + first) * kPitch + at * (8 * sizeof(T) / 4) + i] = w[i];
+    }
+    __syncthreads();
+    if (codes) {                                             // the same for all
+#pragma unroll
+        for (u32 q = 0; q < 8; ++q) {
+            const u32 row = tile_r * 128u + q * 16u + first;
+            const u32 byte = mx_scale_byte<T>(quad_max(mx_peak(v[q])));
+            const u32 code = mx_codes(v[q], byte), four = group_scales(byte);
             if (row < rows) {
                 const u64 o = (u64)row * tiles_c + tile_c;
                 *(u32 *)(codes + o * 64u + at * 4u) = code;
@@ -79,7 +89,6 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize_tile(const T *__restri
             }
         }
     }
-    __syncthreads();
     // four lanes the four blocks of a column (of two, where a word holds two elements): 64 bytes of codes
     const u32 block = threadIdx.x & 3u;
     for (u32 c = threadIdx.x >> 2; c < 128u * sizeof(T) / 4u; c += kThreads / 4u) {
@@ -134,30 +143,42 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize_tile(const T *__restri
     }
 }
 
-// Eight elements a lane.
+// 16 bytes of x a lane: eight elements of a 16-bit type, four floats.  (Eight floats would be two writes a lane whose lanes
+// lie 32 bytes apart: 8192 x 11008 in 109 us against 87.)
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_mx_dequantize(const unsigned char *__restrict__ codes, const unsigned char *__restrict__ scales,
                                                             u32 cols, u32 groups, u32 all, T *__restrict__ x, u64 ld) {
-    constexpr u32 kPieces = 4, kStep = kThreads / 16u;
-    const u32 at = threadIdx.x & 15u;
-    for (u32 first = blockIdx.x * (kStep * kPieces) + threadIdx.x / 16u; first < all; first += gridDim.x * (kStep * kPieces)) {
+    constexpr u32 kEach = 16 / sizeof(T), kLanes = EXCP_MX_GROUP / kEach, kPieces = 4, kStep = kThreads / kLanes;
+    typedef typename std::conditional<kEach == 8, u32, unsigned short>::type Codes;
+    const u32 at = threadIdx.x % kLanes;
+    for (u32 first = blockIdx.x * (kStep * kPieces) + threadIdx.x / kLanes; first < all; first += gridDim.x * (kStep * kPieces)) {
         u32 code[kPieces], byte[kPieces];
 #pragma unroll
         for (u32 q = 0; q < kPieces; ++q) {
             const u32 i = min(first + q * kStep, all - 1u);
-            code[q] = *(const u32 *)(codes + i * 64ull + at * 4u);
-            byte[q] = scales[i * 4ull + at / 4u];
+            code[q] = *(const Codes *)(codes + i * 64ull + at * sizeof(Codes));
+            byte[q] = scales[i * 4ull + at / (kLanes / 4u)];
         }
 #pragma unroll
         for (u32 q = 0; q < kPieces; ++q) {
-            const u32 i = first + q * kStep, row = i / groups, col = (i - row * groups) * EXCP_MX_GROUP + at * 8u;
+            const u32 i = first + q * kStep, row = i / groups, col = (i - row * groups) * EXCP_MX_GROUP + at * kEach;
+            if (i >= all || col >= cols) continue;
             float v[8];
             mx_values(code[q], v);
             const float scale = mx_power(byte[q]);
-            Eight<T> e;
+            T e[kEach];
 #pragma unroll
-            for (u32 j = 0; j < 8; ++j) e.v[j] = (T)(v[j] * scale);
-            if (i < all && col < cols) store_eight(x + row * ld + col, e, cols - col);
+            for (u32 j = 0; j < kEach; ++j) e[j] = (T)(v[j] * scale);
+            T *out = x + row * ld + col;
+            if (col + kEach <= cols) {
+                v4u32 w;
+                __builtin_memcpy(&w, e, 16);
+                *(words_anywhere *)out = w;
+            } else {
+#pragma unroll
+                for (u32 j = 0; j < kEach; ++j)
+                    if (col + j < cols) out[j] = e[j];
+            }
         }
     }
 }
@@ -168,7 +189,8 @@ void in_parts(u32 rows, u32 groups, F f) {
     const u32 most = std::max(1u, (1u << 31) / groups);
     for (u32 r = 0; r < rows; r += std::min(most, rows - r)) f(r, std::min(most, rows - r));
 }
-u32 grid_for(u32 all, u32 cus) { return std::min((all + 63u) / 64u, cus * 16u); }
+// workgroups for `all` groups, `each` at a time
+u32 grid_for(u32 all, u32 each, u32 cus) { return std::min((all + each - 1u) / each, cus * 16u); }
 
 }  // namespace
 
@@ -183,7 +205,7 @@ void launch_mx_quantize(const MxQuantize &q, u32 cus, hipStream_t s) {
         } else {
             in_parts(m.rows, groups, [&](u32 r, u32 rows) {
                 const u32 all = rows * groups;
-                k_mx_quantize<T><<<grid_for(all, cus), kThreads, 0, s>>>((const T *)m.p + (u64)r * m.ld, m.ld, m.cols, groups, all,
+                k_mx_quantize<T><<<grid_for(all, 64u, cus), kThreads, 0, s>>>((const T *)m.p + (u64)r * m.ld, m.ld, m.cols, groups, all,
                                                                          q.codes + (u64)r * groups * 64u, q.scales + (u64)r * groups * 4u);
             });
         }
@@ -196,7 +218,7 @@ void launch_mx_dequantize(const MxDequantize &d, u32 cus, hipStream_t s) {
         using T = decltype(tag);
         in_parts(d.rows, groups, [&](u32 r, u32 rows) {
             const u32 all = rows * groups;
-            k_mx_dequantize<T><<<grid_for(all, cus), kThreads, 0, s>>>(d.codes + (u64)r * groups * 64u, d.scales + (u64)r * groups * 4u, d.cols, groups,
+            k_mx_dequantize<T><<<grid_for(all, sizeof(T) == 2 ? 64u : 32u, cus), kThreads, 0, s>>>(d.codes + (u64)r * groups * 64u, d.scales + (u64)r * groups * 4u, d.cols, groups,
                                                                        all, (T *)d.x + (u64)r * d.ld, d.ld);
         });
     });

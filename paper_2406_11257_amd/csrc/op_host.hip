@@ -28,7 +28,8 @@ u32 groups_of(u64 cols) { return (u32)((cols + EXCP_MX_GROUP - 1) / EXCP_MX_GROU
 // The context's device made current; EXCP_E_HIP where that fails or the context takes no more work.
 int enter(const excp_ctx *c, OpsContext &o) {
     o = excp_ops_context(c);
-    if (o.broken || hipSetDevice(o.device) != hipSuccess) return EXCP_E_HIP;
+    int now = -1;
+    if (o.broken || hipGetDevice(&now) != hipSuccess || (now != o.device && hipSetDevice(o.device) != hipSuccess)) return EXCP_E_HIP;
     return EXCP_OK;
 }
 int launched() { return hipGetLastError() == hipSuccess ? EXCP_OK : EXCP_E_HIP; }
