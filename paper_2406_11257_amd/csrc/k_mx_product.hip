@@ -5,17 +5,18 @@
 
 namespace {
 
-// A tile of WN x WM waves, each 16 TN rows of B (n) by 16 TM rows of A (m); 256 elements of the reduction a stage.
-template <int TN, int TM, int WN, int WM>
+// A tile of WN x WM waves, each 16 TN rows of B (n) by 16 TM rows of A (m); 256 elements of the reduction a stage.  KS such
+// sets of waves share the stages of a workgroup's tile, each with buffers of its own.
+template <int TN, int TM, int WN, int WM, int KS>
 struct Tile {
-    static constexpr u32 bn = 16 * TN * WN, bm = 16 * TM * WM, rows = bn + bm, waves = WN * WM, threads = 64 * waves;
+    static constexpr u32 bn = 16 * TN * WN, bm = 16 * TM * WM, rows = bn + bm, waves = WN * WM, threads = 64 * waves * KS;
     static constexpr u32 codes = rows * 128u, stage = codes + rows * 8u;    // bytes: a row's codes, and its two groups' scales
     static constexpr u32 chunks = rows / 8u / waves;                        // loads a wave: 8 rows of codes each
     static constexpr u32 scale_loads = rows / 32u / waves;                  // and 32 rows of scales each
     static constexpr int loads = chunks + scale_loads;
-    static_assert(rows % (32u * waves) == 0, "");
+    static_assert(rows % (32u * waves) == 0 && (KS - 1) * bn * bm * 4u <= KS * stage, "");
     static constexpr int ahead = 2, before = 2 * TN - (TN + 1) / 2;         // steps (see the kernel)
-    // loads issued before step i of the after + before - gap steps over which they are spread
+    // loads issued before step i of those over which they are spread, counted from the barrier that frees their buffer
     static constexpr int after = 2 * TN - before, spread = 2 * TN - (TN / 2 + 1);
     static constexpr int loaded_by(int i) { return i >= spread ? loads : loads * i / spread; }
     // fragments read before step q begins
@@ -43,17 +44,21 @@ __device__ __forceinline__ void static_for(F f) {
     }
 }
 
-template <class T, int TN, int TM, int WN, int WM>
-__global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) {
-    using L = Tile<TN, TM, WN, WM>;
-    __shared__ __attribute__((aligned(16))) unsigned char even[L::stage], odd[L::stage];
+template <class T, int TN, int TM, int WN, int WM, int KS>
+__global__ __launch_bounds__(64 * WN * WM * KS) void k_mx_product(const MxProduct p) {
+    using L = Tile<TN, TM, WN, WM, KS>;
+    __shared__ __attribute__((aligned(16))) unsigned char even[KS * L::stage], odd[KS * L::stage];
     const u32 lane = lane_id(), r = lane & 15u, g = lane >> 4;
-    const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const u32 any_wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const u32 set = KS > 1 ? any_wave / L::waves : 0u, wave = any_wave - set * L::waves;
     const u32 wn = wave % WN, wm = wave / WN;
     u32 tile_n, tile_m;
     place_of(blockIdx.x, (p.n + L::bn - 1) / L::bn, (p.m + L::bm - 1) / L::bm, tile_n, tile_m);
     const u32 n0 = tile_n * L::bn, m0 = tile_m * L::bm;
-    const u32 groups = p.groups, lone = groups & 1u, stages = groups / 2u;
+    // An odd number of groups leaves one, the first, before the stages; the last round may not have a stage for every set.
+    const u32 groups = p.groups, lone = groups & 1u, stages = groups / 2u, rounds = (stages + KS - 1u) / KS;
+    auto there = [&](u32 t) __attribute__((always_inline)) { return t * KS + set < stages; };
+    auto first_of = [&](u32 t) __attribute__((always_inline)) { return lone + 2u * (t * KS + set); };
 
     // What this wave brings in: rows of codes, eight a load, with the 16-byte pieces of a row permuted so that the
     // sixteen rows of a fragment lie in different banks; and rows of scales, thirty-two a load.  Rows that the matrices
@@ -81,12 +86,12 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
             const u32 chunk = wave * L::chunks + (c - L::scale_loads);
             u32 at = code_at[c - L::scale_loads] - back_codes;
             asm volatile("" : "+v"(at));                     // (as in `hidden`: no pointer a load kept and moved on)
-            load16_to_lds((chunk * 8u < L::bn ? b_codes : a_codes) + first * 64u + at, buf + chunk * 1024u);
+            load16_to_lds((chunk * 8u < L::bn ? b_codes : a_codes) + first * 64u + at, buf + set * L::stage + chunk * 1024u);
         } else {
             const u32 chunk = wave * L::scale_loads + c;
             u32 at = scale_at[c] - back_scales;
             asm volatile("" : "+v"(at));
-            load4_to_lds((chunk * 32u < L::bn ? b_scales : a_scales) + first * 4u + at, buf + L::codes + chunk * 256u);
+            load4_to_lds((chunk * 32u < L::bn ? b_scales : a_scales) + first * 4u + at, buf + set * L::stage + L::codes + chunk * 256u);
         }
     };
     auto fetch = [&](unsigned char *buf, u32 first, u32 back_codes, u32 back_scales) __attribute__((always_inline)) {
@@ -96,8 +101,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
     // Where this lane's parts of the fragments lie.
     struct Places { u32 n[2], m[2], n_scale, m_scale; };
     const u32 swizzled = (g ^ (r & 7u)) * 16u;
-    const Places places = {{rn * 128u + swizzled, rn * 128u + (swizzled ^ 64u)}, {rm * 128u + swizzled, rm * 128u + (swizzled ^ 64u)},
-                           L::codes + rn * 8u + g, L::codes + rm * 8u + g};
+    const u32 base = set * L::stage;
+    const Places places = {{base + rn * 128u + swizzled, base + rn * 128u + (swizzled ^ 64u)}, {base + rm * 128u + swizzled, base + rm * 128u + (swizzled ^ 64u)},
+                           base + L::codes + rn * 8u + g, base + L::codes + rm * 8u + g};
     // The numbers are hidden from the compiler once a stage: it would otherwise keep a register for the address of every
     // fragment of both buffers.
     auto hidden = [&]() __attribute__((always_inline)) {
@@ -128,7 +134,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
         // (the products are not put off until after what follows)
 #pragma unroll
         for (int j = 0; j < TM; ++j) {
-            if constexpr (L::waves > 4) asm volatile("" : "+v"(acc[i][j]));
+            if constexpr (L::threads > 256) asm volatile("" : "+v"(acc[i][j]));
             else asm volatile("" : "+a"(acc[i][j]));
         }
     };
@@ -145,46 +151,65 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
     // Those of the next stage but one begin after the barrier that frees their buffer and end in the next stage.
     auto stage = [&](unsigned char *cur, unsigned char *next, u32 t) __attribute__((always_inline)) {
         const Places at = hidden();
+        const bool here = KS == 1 || there(t);
         static_for<0, L::before>([&](auto q) __attribute__((always_inline)) {
-            if (t + 1u < stages)
+            if (there(t + 1u))
                 static_for<L::loaded_by(L::after + q), L::loaded_by(L::after + q + 1)>([&](auto c) __attribute__((always_inline)) {
-                    load(next, lone + 2u * (t + 1u), 0u, 0u, c);
+                    load(next, first_of(t + 1u), 0u, 0u, c);
                 });
             static_for<L::read_by(q - 1), L::read_by(q)>([&](auto f) __attribute__((always_inline)) { read(cur, at, f); });
             __builtin_amdgcn_sched_barrier(0);
-            step(q);
+            if (here) step(q);
             __builtin_amdgcn_sched_barrier(0);
         });
         landed();                                            // `next` is there, and `cur` has been read by all
         begin(next);                                         // (after the last stage: whatever is there, and unused)
         static_for<L::before, 2 * TN>([&](auto q) __attribute__((always_inline)) {
-            if (t + 2u < stages)
+            if (there(t + 2u))
                 static_for<L::loaded_by(q - L::before), L::loaded_by(q - L::before + 1)>([&](auto c) __attribute__((always_inline)) {
-                    load(cur, lone + 2u * (t + 2u), 0u, 0u, c);
+                    load(cur, first_of(t + 2u), 0u, 0u, c);
                 });
             __builtin_amdgcn_sched_barrier(0);
-            step(q);
+            if (here) step(q);
             __builtin_amdgcn_sched_barrier(0);
         });
     };
     if (lone) {
-        fetch(even, 0, (piece & 4u) * 16u, (lane & 1u) * 4u);
+        if (set == 0) fetch(even, 0, (piece & 4u) * 16u, (lane & 1u) * 4u);
         landed();
-        const Places at = hidden();
-        static_for<0, TM + TN>([&](auto f) __attribute__((always_inline)) { read(even, at, f); });
-        static_for<0, TN>(step);
+        if (set == 0) {
+            const Places at = hidden();
+            static_for<0, TM + TN>([&](auto f) __attribute__((always_inline)) { read(even, at, f); });
+            static_for<0, TN>(step);
+        }
         __syncthreads();
     }
     if (stages) {
-        fetch(even, lone, 0u, 0u);
+        if (there(0)) fetch(even, first_of(0), 0u, 0u);
         landed();
-        if (1u < stages)
-            static_for<0, L::loaded_by(L::after)>([&](auto c) __attribute__((always_inline)) { load(odd, lone + 2u, 0u, 0u, c); });
+        if (there(1u))
+            static_for<0, L::loaded_by(L::after)>([&](auto c) __attribute__((always_inline)) { load(odd, first_of(1u), 0u, 0u, c); });
         begin(even);
-        for (u32 t = 0; t < stages; t += 2u) {
+        for (u32 t = 0; t < rounds; t += 2u) {
             stage(even, odd, t);
-            if (t + 1u < stages) stage(odd, even, t + 1u);
+            if (t + 1u < rounds) stage(odd, even, t + 1u);
         }
+    }
+    if constexpr (KS > 1) {
+        // the sets' sums together, in order, in the first one
+        __syncthreads();
+        v4f32 *const sums = (v4f32 *)even + (wave * TN * TM) * 64u + lane;
+        constexpr u32 of_a_set = L::waves * TN * TM * 64u;
+        if (set) {
+#pragma unroll
+            for (int i = 0; i < TN * TM; ++i) sums[(set - 1u) * of_a_set + i * 64u] = acc[i / TM][i % TM];
+        }
+        __syncthreads();
+        if (set) return;
+#pragma unroll
+        for (u32 other = 0; other < KS - 1u; ++other)
+#pragma unroll
+            for (int i = 0; i < TN * TM; ++i) acc[i / TM][i % TM] += sums[other * of_a_set + i * 64u];
     }
     // A lane holds four consecutive elements of a row of y, sixteen apart.  Of a 16-bit type that would be 32 bytes of a row
     // a write: the lanes of two neighbouring fragments trade halves first, and it is 64.
@@ -209,60 +234,39 @@ __global__ __launch_bounds__(64 * WN * WM) void k_mx_product(const MxProduct p) 
     }
 }
 
-// Few rows of A: the rows of B are read once, each by one wave, and that is the time it takes.  A workgroup has 16 TN rows
-// of B against 16 TM rows of A; its waves take the groups of the reduction in turn (so that together they read runs of a
-// row), straight into registers, BATCH groups on their way at a time, and join their sums in LDS.
-template <class T, int TN, int TM, int BATCH>
+// Up to sixteen rows of A against sixteen rows of B a workgroup: its eight waves take the groups of the reduction in turn
+// (so that together they read runs of a row), straight into registers, four on their way at a time, and join their sums in
+// LDS.  The rows of B are read once, each by one wave, and that is the time it takes.
+template <class T>
 __global__ __launch_bounds__(512) void k_mx_few_rows(const MxProduct p) {
-    constexpr u32 kWaves = 8, kFragments = TN * TM;
-    __shared__ v4f32 part[kWaves][kFragments][64];
-    const u32 lane = lane_id(), r = lane & 15u, g = lane >> 4;
+    constexpr u32 kWaves = 8, kBatch = 4;
+    __shared__ v4f32 sums[kWaves][64];
+    const u32 lane = lane_id(), r = lane & 15u, g = lane >> 4, n0 = blockIdx.x * 16u;
     const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const u32 tiles_n = (p.n + 16u * TN - 1u) / (16u * TN), tiles = tiles_n * ((p.m + 16u * TM - 1u) / (16u * TM));
-    for (u32 tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const u32 n0 = (tile % tiles_n) * 16u * TN, m0 = (tile / tiles_n) * 16u * TM;
-        const unsigned char *row[TN + TM], *scale[TN + TM];
+    const u64 b_row = (u64)min(n0 + r, p.n - 1u) * p.groups, a_row = (u64)min(r, p.m - 1u) * p.groups;
+    v4f32 acc = {};
+    for (u32 first = wave; first < p.groups; first += kWaves * kBatch) {
+        v4i32 b[kBatch], a[kBatch];
+        u32 by_b[kBatch], by_a[kBatch];
 #pragma unroll
-        for (int i = 0; i < TN + TM; ++i) {
-            const u64 at = (u64)(i < TN ? min(n0 + i * 16u + r, p.n - 1u) : min(m0 + (i - TN) * 16u + r, p.m - 1u)) * p.groups;
-            row[i] = (i < TN ? p.b_codes : p.a_codes) + at * 64u + g * 16u;
-            scale[i] = (i < TN ? p.b_scales : p.a_scales) + at * 4u + g;
-        }
-        v4f32 acc[TN][TM] = {};
-        for (u32 first = wave; first < p.groups; first += kWaves * BATCH) {
-            v4i32 codes[BATCH][TN + TM];
-            u32 by[BATCH][TN + TM];
-#pragma unroll
-            for (int u = 0; u < BATCH; ++u) {
-                const u32 k = first + u * kWaves, at = min(k, p.groups - 1u);    // (beyond the last: that one, against zeros)
-#pragma unroll
-                for (int i = 0; i < TN + TM; ++i) {
-                    codes[u][i] = *(const v4i32 *)(row[i] + at * 64ull);
-                    by[u][i] = scale[i][at * 4ull];
-                    if (i >= TN && k >= p.groups) codes[u][i] = v4i32{0, 0, 0, 0};
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < BATCH; ++u)
-#pragma unroll
-                for (int i = 0; i < TN; ++i)
-#pragma unroll
-                    for (int j = 0; j < TM; ++j) acc[i][j] = mx_mfma(codes[u][i], by[u][i], codes[u][TN + j], by[u][TN + j], acc[i][j]);
+        for (u32 u = 0; u < kBatch; ++u) {
+            const u32 k = first + u * kWaves;
+            if (k >= p.groups) continue;
+            b[u] = *(const v4i32 *)(p.b_codes + (b_row + k) * 64u + g * 16u);
+            a[u] = *(const v4i32 *)(p.a_codes + (a_row + k) * 64u + g * 16u);
+            by_b[u] = p.b_scales[(b_row + k) * 4u + g];
+            by_a[u] = p.a_scales[(a_row + k) * 4u + g];
         }
 #pragma unroll
-        for (int i = 0; i < TN; ++i)
-#pragma unroll
-            for (int j = 0; j < TM; ++j) part[wave][i * TM + j][lane] = acc[i][j];
-        __syncthreads();
-        for (u32 f = wave; f < kFragments; f += kWaves) {
-            v4f32 sum = part[0][f][lane];
-#pragma unroll
-            for (u32 w = 1; w < kWaves; ++w) sum += part[w][f][lane];
-            const u32 n = n0 + (f / TM) * 16u + g * 4u, m = m0 + (f % TM) * 16u + r;
-            if (m < p.m) store_four((T *)p.y + (u64)m * p.ld, n, p.n, sum);
-        }
-        __syncthreads();
+        for (u32 u = 0; u < kBatch; ++u)
+            if (first + u * kWaves < p.groups) acc = mx_mfma(b[u], by_b[u], a[u], by_a[u], acc);
     }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (u32 i = 1; i < kWaves; ++i) acc += sums[i][lane];
+    if (r < p.m) store_four((T *)p.y + (u64)r * p.ld, n0 + g * 4u, p.n, acc);
 }
 
 // The same for up to sixteen rows of x that are quantised on the way: once a workgroup, into LDS (a part of the reduction at
@@ -344,11 +348,6 @@ __global__ __launch_bounds__(512) void k_mx_few_rows_of(const MxProduct p, u32 r
     }
 }
 
-template <class T, int TN, int TM, int BATCH>
-void launch_few(const MxProduct &p, hipStream_t s) {
-    const u32 tiles = ((p.n + 16u * TN - 1u) / (16u * TN)) * ((p.m + 16u * TM - 1u) / (16u * TM));
-    k_mx_few_rows<T, TN, TM, BATCH><<<std::min(tiles, 1u << 20), 512, 0, s>>>(p);
-}
 template <class X, class T>
 void launch_few_of(const MxProduct &p, u32 cus, hipStream_t s) {
     // LDS: a group of x takes 68 bytes a row; with the sums, 64 KB, so that a compute unit has two workgroups
@@ -356,28 +355,30 @@ void launch_few_of(const MxProduct &p, u32 cus, hipStream_t s) {
     k_mx_few_rows_of<X, T><<<std::min((p.n + 15u) / 16u, 2u * cus), 512, room * p.m * 68u, s>>>(p, room);
 }
 
-}  // namespace
-
-template <class T, int TN, int TM, int WN, int WM>
+template <class T, int TN, int TM, int WN, int WM, int KS>
 void launch_tiles(const MxProduct &p, hipStream_t s) {
-    using L = Tile<TN, TM, WN, WM>;
-    const u64 tiles = (u64)((p.n + L::bn - 1) / L::bn) * ((p.m + L::bm - 1) / L::bm);
-    k_mx_product<T, TN, TM, WN, WM><<<(u32)tiles, L::threads, 0, s>>>(p);
+    using L = Tile<TN, TM, WN, WM, KS>;
+    const u32 tiles = ((p.n + L::bn - 1) / L::bn) * ((p.m + L::bm - 1) / L::bm);
+    k_mx_product<T, TN, TM, WN, WM, KS><<<tiles, L::threads, 0, s>>>(p);
 }
 
+}  // namespace
+
 void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
+    // The largest tile that gives three workgroups in four compute units and more (a tile's rows are read once for the whole
+    // of the other side); where there are no more of the smallest than compute units, four sets of waves a tile.  Measured,
+    // m x n x k: 8192 x 8192 x 8192 in tiles of 256: 290 us; 4096 x 2048 x 8192 in 128 tiles of 256: 61 us, of 128: 49;
+    // 1000 x 2000 x 3000 in tiles of 64: 10 us; 100 x 1024 x 11008 with four sets 18 us, with one 26, and 512 x 4096 x 4096,
+    // 512 tiles, 13 us either way.
+    auto tiles = [&](u32 n, u32 m) { return (u64)((p.n + n - 1u) / n) * ((p.m + m - 1u) / m); };
     with_type(p.type, [&](auto tag) {
         using T = decltype(tag);
-        if (p.m <= 64u) {
-            if (p.m <= 16u) launch_few<T, 1, 1, 4>(p, s);
-            else if (p.m <= 32u) launch_few<T, 2, 2, 2>(p, s);
-            else launch_few<T, 1, 4, 2>(p, s);
-            return;
-        }
-        const u64 large = (u64)((p.n + 255u) / 256u) * ((p.m + 255u) / 256u), middle = (u64)((p.n + 127u) / 128u) * ((p.m + 127u) / 128u);
-        if (large >= cus * 3 / 4) launch_tiles<T, 8, 4, 2, 4>(p, s);
-        else if (middle >= cus * 3 / 4) launch_tiles<T, 4, 4, 2, 2>(p, s);
-        else launch_tiles<T, 2, 2, 2, 2>(p, s);
+        // (16 x 4096 x 4096: 6.1 us, in tiles 7.6; 16 x 50304 x 2048 in tiles 21 us, so 48)
+        if (p.m <= 16u && p.n <= 32u * cus) k_mx_few_rows<T><<<(p.n + 15u) / 16u, 512, 0, s>>>(p);
+        else if (tiles(256u, 256u) >= cus * 3 / 4) launch_tiles<T, 8, 4, 2, 4, 1>(p, s);
+        else if (tiles(128u, 128u) >= cus * 3 / 4) launch_tiles<T, 4, 4, 2, 2, 1>(p, s);
+        else if (tiles(64u, 64u) > cus) launch_tiles<T, 2, 2, 2, 2, 1>(p, s);
+        else launch_tiles<T, 2, 2, 2, 2, 4>(p, s);
     });
 }
 

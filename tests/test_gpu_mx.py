@@ -132,7 +132,8 @@ def product_bound(a, b, dtype):
 
 PRODUCTS = [(1, 1, 1), (1, 16, 128), (1, 17, 129), (2, 1000, 32), (15, 33, 1000), (16, 256, 512), (17, 65, 384), (33, 130, 130),
             (64, 64, 64), (128, 128, 128), (129, 127, 257), (200, 300, 640), (256, 256, 1024), (257, 511, 300), (333, 1031, 1000),
-            (48, 2048, 4096), (1000, 24, 2500), (16, 100, 9000), (9, 70, 20001), (1, 40, 120000), (16, 9000, 700)]
+            (48, 2048, 4096), (1000, 24, 2500), (16, 100, 9000), (9, 70, 20001), (1, 40, 120000), (16, 9000, 700),
+            (70, 200, 1152), (64, 64, 1280), (100, 90, 3000), (17, 40, 256), (128, 66, 128), (50, 4000, 2176)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
