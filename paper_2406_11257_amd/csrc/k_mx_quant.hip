@@ -1,6 +1,9 @@
 // Microscaled 4-bit floating point: quantisation along the rows and down the columns of a matrix, and back.
 //
-// All three are bound by memory: 2 or 4 bytes an element one way, 0.53 the other.
+// The scale of a block of 32 is the power of two whose exponent is that of its largest magnitude less 2 (6, the largest
+// element, is 1.5 x 2^2); the conversion instructions divide by it, round to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6, ties to
+// the even code, and saturate.  All kernels here are bound by memory: 2 or 4 bytes an element one way, 0.53 the other.
+// 11008 x 4096 in bf16: 27 us there (4.2 TB/s) and 18 back (6.3); along and down at once 4096 x 8192: 25 us (4.1).
 #include "excp_ops_device.h"
 
 #include <type_traits>
@@ -21,8 +24,9 @@ __device__ __forceinline__ u32 group_scales(u32 byte) {
     return v | dpp_u32<0x128, 0xf>(0u, v);
 }
 
-// Sixteen lanes a group, eight elements each; codes and scales lie group after group, whatever the rows.  A thread has
-// pieces of four groups under way.
+// Sixteen lanes a group, eight elements each, so that a wave reads and writes whole lines and a block's largest is found by
+// four neighbours; codes and scales lie group after group, whatever the rows.  A thread has pieces of four groups under way.
+// (One row of 1024 takes 3 us, the launch; 11008 x 4096 in bf16 27 us out of memory, 20 where the last-level cache has it.)
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_mx_quantize(const T *__restrict__ x, u64 ld, u32 cols, u32 groups, u32 all,
                                                           unsigned char *__restrict__ codes, unsigned char *__restrict__ scales) {
@@ -47,7 +51,8 @@ __global__ __launch_bounds__(kThreads) void k_mx_quantize(const T *__restrict__ 
     }
 }
 
-// A tile of 128 x 128 elements a workgroup: quantised along its rows on the way in, and from LDS down its columns.
+// A tile of 128 x 128 elements a workgroup: quantised along its rows on the way in, and from LDS down its columns, so that x is
+// read once for both.  All of a tile's reads are on their way before the first is used.
 template <class T>
 struct TileRoom {
     static constexpr u32 pitch = 128 * sizeof(T) / 4 + 1;    // in words
