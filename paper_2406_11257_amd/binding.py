@@ -500,9 +500,9 @@ class Context:
         gpu = self.device.index
         ptr, kind, rows, cols, ld = _matrix(x, "x", gpu)
         c = s = ct = st = None
-        if codes is not None:
+        if codes is not None or scales is not None:
             c, s = _coded(codes, scales, rows, cols, "the rows'", gpu)
-        if codes_t is not None:
+        if codes_t is not None or scales_t is not None:
             ct, st = _coded(codes_t, scales_t, cols, rows, "the columns'", gpu)
         rc = lib().excp_mx_quantize(self._h, ptr, kind, rows, cols, ld, c, s, ct, st)
         if rc != EXCP_OK:
@@ -537,7 +537,7 @@ class Context:
             raise ValueError("x and y differ in rows")
         w, sw = _coded(w_codes, w_scales, n, k, "W's", gpu)
         c = s = None
-        if x_codes is not None:
+        if x_codes is not None or x_scales is not None:
             c, s = _coded(x_codes, x_scales, m, k, "x's", gpu)
         rc = lib().excp_mx_linear(self._h, xp, xkind, ldx, w, sw, m, n, k, yp, ykind, ldy, c, s)
         if rc != EXCP_OK:

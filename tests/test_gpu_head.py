@@ -67,6 +67,35 @@ def test_a_head_that_was_not_made_to_train():
     ctx.close()
 
 
+def test_a_context_on_another_stream():
+    """Work queued before a call is waited for, and what follows a call waits for it, whatever stream each is on."""
+    here, own = X.Context(4096), torch.cuda.Stream()
+    own.wait_stream(torch.cuda.current_stream())
+    there = X.Context(4096, stream=own)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    w0, h0 = (torch.empty(n, 256, device="cuda").normal_(generator=g) for n in (4099, 300))
+    t = torch.randint(0, 4099, (300,), device="cuda", generator=g)
+    ones = torch.ones(300, device="cuda")
+    big = torch.empty(4096, 8192, device="cuda")
+    results = []
+    for ctx in (here, there):
+        for _ in range(20):
+            big.normal_()                                    # keeps the caller's stream busy
+        w, h = w0 * 0.5, h0 + 0.0
+        hd = head.MxHead(ctx, w, train=True)
+        del w
+        torch.empty(4099, 256, device="cuda").fill_(7.0)
+        s = hd.score(h, t, 3)
+        scored = [s[k].clone() for k in ("logits", "logprob", "entropy", "top_ids")]
+        dh, dw = hd.gradients(h, t, s, ones)
+        results.append(scored + [dh + 0.0, dw + 0.0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    here.close()
+    there.close()
+
+
 def test_the_command():
     r = head.compare(0, 64)
     assert r["same_first"] > 0.9 and abs(r["logprob"][0] - r["logprob"][1]) < 0.1 and r["compressed"] > 8

@@ -326,3 +326,12 @@ def test_refusals(ctx):
         ctx.excp_mx_quantize(x)
     with pytest.raises(X.ExcpError):
         ctx.excp_mx_linear(x, c, s, y)
+
+
+def test_scales_without_codes_are_refused(ctx):
+    x, y = torch.zeros(4, 256, device="cuda"), torch.zeros(4, 64, device="cuda")
+    (c, s), (ct, st), (w, sw) = X.mx_empty(4, 256), X.mx_empty(256, 4), X.mx_empty(64, 256)
+    for call in (lambda: ctx.excp_mx_quantize(x, None, s, ct, st), lambda: ctx.excp_mx_quantize(x, c, s, None, st),
+                 lambda: ctx.excp_mx_linear(x, w, sw, y, None, s)):
+        with pytest.raises(TypeError):
+            call()
