@@ -384,14 +384,18 @@ void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
     // of the other side); where there are no more of the smallest than compute units, four sets of waves a tile.  Measured,
     // m x n x k: 8192 x 8192 x 8192 in tiles of 256: 290 us; 4096 x 2048 x 8192 in 128 tiles of 256: 61 us, of 128: 49;
     // 1000 x 2000 x 3000 in tiles of 64: 10 us; 100 x 1024 x 11008 with four sets 18 us, with one 26, and 512 x 4096 x 4096,
-    // 512 tiles, 13 us either way.
+    // 512 tiles, 13 us either way.  Of m no more than half of a tile is left empty (32 x 32000 x 4096 in tiles of 128: 22.4 us,
+    // of 64: 18.7; 128 x 50304 x 2048 in tiles of 256: 23.5, of 128: 21.0; but 130 x 50304 x 4096: 39 and 51).  Up to 64 rows
+    // are bound by the read of B, which two sets of waves keep going where it is long: 64 x 22016 x 4096 21.2 us with one and
+    // 19.1 with two, 40 x 50304 x 4096 33.9 and 30.2, 60 x 50304 x 1024 9.1 and 11.5.
     auto tiles = [&](u32 n, u32 m) { return (u64)((p.n + n - 1u) / n) * ((p.m + m - 1u) / m); };
     with_type(p.type, [&](auto tag) {
         using T = decltype(tag);
-        // (16 x 4096 x 4096: 6.1 us, in tiles 7.6; 16 x 50304 x 2048 in tiles 21 us, not in tiles 48)
+        // (16 x 4096 x 4096: 6.1 us, in tiles 7.6; 16 x 50304 x 2048 in tiles 14 us, not in tiles 48)
         if (p.m <= 16u && p.n <= 32u * cus) k_mx_few_rows<T><<<(p.n + 15u) / 16u, 512, 0, s>>>(p);
-        else if (tiles(256u, 256u) >= cus * 3 / 4) launch_tiles<T, 8, 4, 2, 4, 1>(p, s);
-        else if (tiles(128u, 128u) >= cus * 3 / 4) launch_tiles<T, 4, 4, 2, 2, 1>(p, s);
+        else if (p.m > 128u && tiles(256u, 256u) >= cus * 3 / 4) launch_tiles<T, 8, 4, 2, 4, 1>(p, s);
+        else if (p.m > 64u && tiles(128u, 128u) >= cus * 3 / 4) launch_tiles<T, 4, 4, 2, 2, 1>(p, s);
+        else if (p.m <= 64u && p.groups >= 32u && tiles(64u, 64u) > cus) launch_tiles<T, 2, 4, 2, 1, 2>(p, s);
         else if (tiles(64u, 64u) > cus) launch_tiles<T, 2, 2, 2, 2, 1>(p, s);
         else launch_tiles<T, 2, 2, 2, 2, 4>(p, s);
     });

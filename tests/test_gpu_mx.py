@@ -335,3 +335,24 @@ def test_scales_without_codes_are_refused(ctx):
                  lambda: ctx.excp_mx_linear(x, w, sw, y, None, s)):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("dtype,gap", [("f32", 3), ("bf16", 0), ("f16", 8)])
+@pytest.mark.parametrize("m,n,k", [(40, 16500, 4096), (64, 16449, 4200), (17, 20011, 5100), (1, 17000, 4224), (33, 16390, 8000), (63, 25000, 700),
+                                   (16, 16400, 130), (100, 25001, 300), (128, 24700, 1000), (65, 24600, 4097), (129, 50000, 256)])
+def test_matmul_of_few_rows_by_many(ctx, m, n, k, dtype, gap):
+    """A few rows against so many that the GPU is full (compared in 64 bits on the GPU)."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(m + n + k)
+    (ca, cb), values = (X.mx_empty(m, k), X.mx_empty(n, k)), []
+    for (codes, scales), rows, scale in ((ca, m, 1.0), (cb, n, 0.02)):
+        a = torch.empty(rows, k, device="cuda").normal_(0, scale, generator=g)
+        ctx.excp_mx_quantize(a, codes, scales)
+        ctx.excp_mx_dequantize(codes, scales, a)
+        values.append(a.double())
+    whole = torch.full((m, n + gap), 9.0, dtype=DTYPES[dtype], device="cuda")
+    y = whole[:, :n]
+    ctx.excp_mx_matmul(*ca, *cb, k, y)
+    want, size = values[0] @ values[1].t(), values[0].abs() @ values[1].abs().t()
+    bound = (-(-k // 128) + 16) * 2.0 ** -22 * size + HALF_ULP[dtype] * size + SMALLEST[dtype]
+    assert bool(((y.double() - want).abs() <= bound).all()) and bool((whole[:, n:] == 9.0).all())
