@@ -56,7 +56,7 @@ __device__ __forceinline__ void static_for(F f) {
 // 16 TM rows, so that each byte read from LDS is used TN or TM times: waves of 128 x 64 in a tile of 256 x 256, which the
 // registers hold with two waves a SIMD.  (Tried: 128 x 128 a wave, one wave a SIMD, 324 us for 8192 x 8192 x 8192; the 32 x 32
 // shape of the unit, 319; a workgroup that goes on to another tile with its first stages on their way while the last is
-// written, 297; writes past the caches, 302.)
+// written, 302; writes past the caches, 302.)
 template <class T, int TN, int TM, int WN, int WM, int KS>
 __global__ __launch_bounds__(64 * WN * WM * KS) void k_mx_product(const MxProduct p) {
     using L = Tile<TN, TM, WN, WM, KS>;
