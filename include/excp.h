@@ -364,8 +364,8 @@ int excp_mx_dequantize(excp_ctx *ctx, const void *codes, const void *scales, uin
 int excp_mx_matmul(excp_ctx *ctx, const void *a_codes, const void *a_scales, const void *b_codes,
                    const void *b_scales, uint64_t m, uint64_t n, uint64_t k, void *y, int type, uint64_t ld);
 
-/* y (m x n) = MX(x) W^T for x in 16 or 32 bits: excp_mx_quantize of x and excp_mx_matmul in one call (for
- * few rows in one kernel, whose fp32 sums go in another order).  x_codes and x_scales (sizes as above for
+/* y (m x n) = MX(x) W^T for x in 16 or 32 bits: excp_mx_quantize of x and excp_mx_matmul in one call (few
+ * rows may go in one kernel, whose fp32 sums are in another order).  x_codes and x_scales (sizes as above for
  * m x k) are room to work in; what they hold afterwards is unspecified.  They may be NULL for up to
  * EXCP_MX_FEW_ROWS rows, which need none. */
 #define EXCP_MX_FEW_ROWS 16

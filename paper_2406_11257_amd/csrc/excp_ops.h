@@ -15,7 +15,7 @@ struct OpsContext {
     int device;
     hipStream_t stream;
     u32 cus;               // compute units
-    RowPart *parts;        // EXCP_ROW_PARTS records of rows that several workgroups share
+    RowPart *parts;        // EXCP_ROW_PARTS records of rows that several workgroups share; or room for a few rows' codes
     u32 *tickets;          // as many counters, zero between calls
     bool broken;
 };
@@ -64,6 +64,7 @@ void launch_mx_quantize(const MxQuantize &q, u32 cus, hipStream_t s);
 void launch_mx_dequantize(const MxDequantize &d, u32 cus, hipStream_t s);
 void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s);
 void launch_mx_few_rows(const MxProduct &p, u32 cus, hipStream_t s);
+bool mx_quantized_first(const MxProduct &p, u32 cus);   // whether a few rows of x are better quantised in a launch of their own
 void launch_row_scores(const RowScores &r, const OpsContext &c);
 void launch_row_gradient(const RowGradient &r, u32 cus, hipStream_t s);
 

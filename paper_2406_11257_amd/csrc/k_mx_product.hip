@@ -285,8 +285,8 @@ __global__ __launch_bounds__(512) void k_mx_few_rows(const MxProduct p) {
 // The same for up to sixteen rows of x that are quantised on the way: once a workgroup, into LDS (a part of the reduction at
 // a time, where all of it does not fit), and from there against tile after tile of sixteen rows of W.  What lanes of rows that
 // x does not have read is another row's: nobody reads their sums.
-// One row by 4096 x 4096 takes 4.7 us (quantised by every wave for itself, 6.8), of which W's bytes are 1.8; sixteen by
-// 50304 x 2048 18 us, W and y 11.
+// One row by 4096 x 4096 takes 4.7 us (quantised by every wave for itself, 6.8), of which W's bytes are 1.8; by 50304 x 4096
+// 26.6, W 21.
 template <class X, class T>
 __global__ __launch_bounds__(512) void k_mx_few_rows_of(const MxProduct p, u32 room) {
     constexpr u32 kWaves = 8, kBatch = 4;
@@ -363,10 +363,11 @@ __global__ __launch_bounds__(512) void k_mx_few_rows_of(const MxProduct p, u32 r
     }
 }
 
+// Groups of m rows of x in LDS, 68 bytes a row each: with the sums 64 KB, so that a compute unit has two workgroups.
+u32 few_room(u32 m) { return 57344u / (68u * m); }
 template <class X, class T>
 void launch_few_of(const MxProduct &p, u32 cus, hipStream_t s) {
-    // LDS: a group of x takes 68 bytes a row; with the sums, 64 KB, so that a compute unit has two workgroups
-    const u32 room = std::min(p.groups, 57344u / (68u * p.m));
+    const u32 room = std::min(p.groups, few_room(p.m));
     k_mx_few_rows_of<X, T><<<std::min((p.n + 15u) / 16u, 2u * cus), 512, room * p.m * 68u, s>>>(p, room);
 }
 
@@ -401,6 +402,13 @@ void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
     });
 }
 
+bool mx_quantized_first(const MxProduct &p, u32 cus) {
+    // Where x does not fit in LDS as a whole, it would be quantised again for every tile of sixteen rows of W (16 x 32000 x
+    // 8192: 78 us in one launch, 36 in two; 16 x 4096 x 11008: 16.3 and 13.7); and where W's rows fill the GPU with tiles of 64,
+    // those read it faster (8 x 22016 x 4096: 18.5 and 16.4; 16 x 50304 x 2048: 19.7 and 16.7), by more than the second launch
+    // takes if there are more than four rows (4 x 22016 x 4096: 15.1 and 16.2; 1 x 50304 x 4096: 26.6 and 28.9).
+    return p.groups > few_room(p.m) || (p.m > 4u && p.n >= 64u * cus);
+}
 void launch_mx_few_rows(const MxProduct &p, u32 cus, hipStream_t s) {
     with_type(p.x.type, [&](auto xtag) { with_type(p.type, [&](auto tag) { launch_few_of<decltype(xtag), decltype(tag)>(p, cus, s); }); });
 }

@@ -356,3 +356,26 @@ def test_matmul_of_few_rows_by_many(ctx, m, n, k, dtype, gap):
     want, size = values[0] @ values[1].t(), values[0].abs() @ values[1].abs().t()
     bound = (-(-k // 128) + 16) * 2.0 ** -22 * size + HALF_ULP[dtype] * size + SMALLEST[dtype]
     assert bool(((y.double() - want).abs() <= bound).all()) and bool((whole[:, n:] == 9.0).all())
+
+
+@pytest.mark.parametrize("xtype,ytype", [("f32", "f32"), ("bf16", "f16")])
+@pytest.mark.parametrize("m,n,k", [(16, 40, 6657), (16, 500, 11008), (12, 33, 9001), (5, 16500, 129), (16, 17000, 300), (4, 17000, 300), (9, 16384, 0),
+                                   (16, 20, 63488), (16, 18, 63489), (13, 34, 90000), (7, 300, 33000)])
+def test_few_rows_of_any_length(ctx, m, n, k, xtype, ytype):
+    """One to sixteen rows that fit where they are quantised, or not, against few rows of W and many; with room given and without."""
+    x = draw(m, k, xtype, m + k, 1.0)
+    a = mx_values(*mx_reference(x), k) if k else x
+    cb, b = coded(draw(n, k, "f32", n + k + 1, 0.02)) if k else (X.mx_empty(n, 0), np.zeros((n, 0)))
+    y = strided(np.full((m, n), 9.0), ytype, 3, 0)
+    ctx.excp_mx_linear(strided(x, xtype, 1, 1), *cb, y)
+    assert (np.abs(f64(y) - a @ b.T) <= product_bound(a, b, ytype)).all()
+    again = torch.full((m, n), 9.0, dtype=DTYPES[ytype], device="cuda")
+    ctx.excp_mx_linear(strided(x, xtype), *cb, again, *X.mx_empty(m, k))
+    assert torch.equal(again, y)
+    # the room is that of rows of logits: neither harms the other
+    logits = torch.linspace(-3, 3, 70001, device="cuda").repeat(2, 1)
+    ids, lp = torch.empty(2, 4, dtype=torch.int64, device="cuda"), torch.empty(2, 4, device="cuda")
+    for _ in range(3):
+        ctx.excp_mx_linear(strided(x, xtype), *cb, again)
+        ctx.excp_token_logprobs(logits, top_logprob=lp, top_ids=ids)
+        assert torch.equal(again, y) and ids[1].tolist() == [70000, 69999, 69998, 69997]
