@@ -25,12 +25,12 @@ __device__ __forceinline__ u32 group_scales(u32 byte) {
 }
 
 // Sixteen lanes a group, eight elements each, so that a wave reads and writes whole lines and a block's largest is found by
-// four neighbours; codes and scales lie group after group, whatever the rows.  A thread has pieces of four groups under way.
-// (One row of 1024 takes 3 us, the launch; 11008 x 4096 in bf16 27 us out of memory, 20 where the last-level cache has it.)
-template <class T>
+// four neighbours; codes and scales lie group after group, whatever the rows.  A thread has `kPieces` pieces of
+// groups under way.  (One row of 1024 takes 2 us, the launch; 11008 x 4096 in bf16 27 us out of memory, 20 where the last-level cache has it.)
+template <class T, u32 kPieces>
 __global__ __launch_bounds__(kThreads) void k_mx_quantize(const T *__restrict__ x, u64 ld, u32 cols, u32 groups, u32 all,
                                                           unsigned char *__restrict__ codes, unsigned char *__restrict__ scales) {
-    constexpr u32 kPieces = 4, kStep = kThreads / 16u;
+    constexpr u32 kStep = kThreads / 16u;
     const u32 at = threadIdx.x & 15u;
     for (u32 first = blockIdx.x * (kStep * kPieces) + threadIdx.x / 16u; first < all; first += gridDim.x * (kStep * kPieces)) {
         Eight<T> v[kPieces];
@@ -210,8 +210,14 @@ void launch_mx_quantize(const MxQuantize &q, u32 cus, hipStream_t s) {
         } else {
             in_parts(m.rows, groups, [&](u32 r, u32 rows) {
                 const u32 all = rows * groups;
-                k_mx_quantize<T><<<grid_for(all, 64u, cus), kThreads, 0, s>>>((const T *)m.p + (u64)r * m.ld, m.ld, m.cols, groups, all,
+                auto go = [&](auto kernel, u32 each) {
+                    kernel<<<grid_for(all, each, cus), kThreads, 0, s>>>((const T *)m.p + (u64)r * m.ld, m.ld, m.cols, groups, all,
                                                                          q.codes + (u64)r * groups * 64u, q.scales + (u64)r * groups * 4u);
+                };
+                // few groups on as many compute units as there are (333 x 1000 in fp16: 3.4 us, four pieces a thread 4.6; 512 x
+                // 4096, four times as many as may be, 4.5 either way)
+                if (all <= 16u * cus) go(k_mx_quantize<T, 1>, 16u);
+                else go(k_mx_quantize<T, 4>, 64u);
             });
         }
     });
