@@ -213,12 +213,14 @@ def excp_decompress_step_static(Wp, blob, blob_bytes, W_recon_out=None, m_out=No
 
 _types = {}
 _uint8 = _int64 = _float32 = None
+_wider = ()
 
 
 def _load_types():
-    global _uint8, _int64, _float32
+    global _uint8, _int64, _float32, _wider
     import torch
     _uint8, _int64, _float32 = torch.uint8, torch.int64, torch.float32
+    _wider = (torch.int64, torch.int32, torch.int16)
     _types.update({torch.float32: EXCP_TYPE_F32, torch.float16: EXCP_TYPE_F16, torch.bfloat16: EXCP_TYPE_BF16})
 
 
@@ -251,6 +253,17 @@ def _coded(codes, scales, rows, cols, name, gpu):
         raise TypeError(f"{name} codes and scales must be contiguous uint8 tensors of shapes {(rows, groups * 64)} and "
                         f"{(rows, groups * 4)} on cuda:{gpu}")
     return codes.data_ptr(), scales.data_ptr()
+
+
+def _as_bytes(t, stream):
+    """Codes or scales that a call reads, as the bytes that the library stores.  Arithmetic on bytes soon yields a wider
+    integer type (8 * a truth value is int64); whole numbers from 0 to 255 in one are brought to bytes on the context's
+    stream.  What is to be written, and anything else, stays what it is."""
+    if t is None or t.dtype is _uint8 or t.dtype not in _wider or not t.is_cuda or not t.is_contiguous():
+        return t
+    import torch
+    with torch.cuda.stream(stream):
+        return t.to(_uint8)
 
 
 def mx_empty(rows: int, cols: int, device="cuda"):
@@ -509,18 +522,22 @@ class Context:
             raise ExcpError(rc, "excp_mx_quantize")
 
     def excp_mx_dequantize(self, codes, scales, x):
-        """The values of codes and scales into the matrix x."""
+        """The values of codes and scales (bytes, or whole numbers from 0 to 255 in int16, int32 or int64) into the matrix x."""
         gpu = self.device.index
         ptr, kind, rows, cols, ld = _matrix(x, "x", gpu)
+        codes, scales = _as_bytes(codes, self._stream), _as_bytes(scales, self._stream)
         c, s = _coded(codes, scales, rows, cols, "x's", gpu)
         rc = lib().excp_mx_dequantize(self._h, c, s, rows, cols, ptr, kind, ld)
         if rc != EXCP_OK:
             raise ExcpError(rc, "excp_mx_dequantize")
 
     def excp_mx_matmul(self, a_codes, a_scales, b_codes, b_scales, k, y):
-        """y (m x n) = A B^T of A (m x k) and B (n x k) in codes and scales."""
+        """y (m x n) = A B^T of A (m x k) and B (n x k) in codes and scales (bytes, or whole numbers from 0 to 255 in
+        int16, int32 or int64, which each call brings to bytes first)."""
         gpu = self.device.index
         ptr, kind, m, n, ld = _matrix(y, "y", gpu)
+        a_codes, a_scales = _as_bytes(a_codes, self._stream), _as_bytes(a_scales, self._stream)
+        b_codes, b_scales = _as_bytes(b_codes, self._stream), _as_bytes(b_scales, self._stream)
         a, sa = _coded(a_codes, a_scales, m, k, "A's", gpu)
         b, sb = _coded(b_codes, b_scales, n, k, "B's", gpu)
         rc = lib().excp_mx_matmul(self._h, a, sa, b, sb, m, n, k, ptr, kind, ld)
@@ -528,13 +545,15 @@ class Context:
             raise ExcpError(rc, "excp_mx_matmul")
 
     def excp_mx_linear(self, x, w_codes, w_scales, y, x_codes=None, x_scales=None):
-        """y (m x n) = MX(x) W^T; x_codes and x_scales (as mx_empty makes them for x) are room to work in, not needed
-        for up to EXCP_MX_FEW_ROWS rows."""
+        """y (m x n) = MX(x) W^T of W (n x k) in codes and scales (bytes, or whole numbers from 0 to 255 in int16, int32
+        or int64, which each call brings to bytes first); x_codes and x_scales (as mx_empty makes them for x) are room to
+        work in, not needed for up to EXCP_MX_FEW_ROWS rows."""
         gpu = self.device.index
         xp, xkind, m, k, ldx = _matrix(x, "x", gpu)
         yp, ykind, my, n, ldy = _matrix(y, "y", gpu)
         if my != m:
             raise ValueError("x and y differ in rows")
+        w_codes, w_scales = _as_bytes(w_codes, self._stream), _as_bytes(w_scales, self._stream)
         w, sw = _coded(w_codes, w_scales, n, k, "W's", gpu)
         c = s = None
         if x_codes is not None or x_scales is not None:

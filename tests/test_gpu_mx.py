@@ -379,3 +379,48 @@ def test_few_rows_of_any_length(ctx, m, n, k, xtype, ytype):
         ctx.excp_mx_linear(strided(x, xtype), *cb, again)
         ctx.excp_token_logprobs(logits, top_logprob=lp, top_ids=ids)
         assert torch.equal(again, y) and ids[1].tolist() == [70000, 69999, 69998, 69997]
+
+
+@pytest.mark.parametrize("wide", [torch.int16, torch.int32, torch.int64])
+def test_codes_in_a_wider_integer_type(ctx, wide):
+    """Codes made by integer arithmetic, which promotes bytes: what reads them brings them back, on the context's stream."""
+    (ca, _), (cb, _) = coded(draw(40, 700, "f32", 1, 1.0)), coded(draw(300, 700, "f32", 2))
+    wa, wb = ([t.to(wide) for t in q] for q in (ca, cb))
+    x = strided(draw(40, 700, "f32", 3, 1.0), "f32")
+    y, z = torch.empty(40, 300, device="cuda"), torch.empty(40, 300, device="cuda")
+    ctx.excp_mx_matmul(*ca, *cb, 700, y)
+    for a, b in ((wa, wb), (ca, wb), ([wa[0], ca[1]], [cb[0], wb[1]])):
+        ctx.excp_mx_matmul(*a, *b, 700, z.fill_(9.0))
+        assert torch.equal(y, z)
+    for rows in (1, 16, 40):
+        ctx.excp_mx_linear(x[:rows], *cb, y[:rows], *X.mx_empty(rows, 700))
+        ctx.excp_mx_linear(x[:rows], *wb, z[:rows].fill_(9.0), *X.mx_empty(rows, 700))
+        assert torch.equal(y[:rows], z[:rows])
+    v, w = torch.empty(300, 700, device="cuda"), torch.empty(300, 700, device="cuda")
+    ctx.excp_mx_dequantize(*cb, v)
+    ctx.excp_mx_dequantize(*wb, w)
+    assert torch.equal(v, w)
+    own, big, room, more = torch.cuda.Stream(), torch.empty(4096, 8192, device="cuda"), X.mx_empty(40, 700), X.mx_empty(40, 700)
+    own.wait_stream(torch.cuda.current_stream())
+    there = X.Context(4096, stream=own)
+    with torch.cuda.stream(own):
+        for _ in range(10):
+            big.normal_()
+        late = [t + 0 for t in wb]                           # not there yet when the call is made
+    there.excp_mx_linear(x, *late, z, *room)
+    ctx.excp_mx_linear(x, *cb, y, *more)
+    torch.cuda.synchronize()
+    assert torch.equal(y, z)
+    there.close()
+
+
+def test_codes_that_are_no_bytes_are_refused(ctx):
+    x, y = torch.zeros(4, 256, device="cuda"), torch.zeros(4, 64, device="cuda")
+    (w, sw), (c, s) = X.mx_empty(64, 256), X.mx_empty(4, 256)
+    for call in (lambda: ctx.excp_mx_linear(x, w.float(), sw, y), lambda: ctx.excp_mx_linear(x, w.bool(), sw, y),
+                 lambda: ctx.excp_mx_linear(x, w.long()[:63], sw, y), lambda: ctx.excp_mx_linear(x, w.long().cpu(), sw, y),
+                 lambda: ctx.excp_mx_linear(x, w.long()[:, ::2], sw, y), lambda: ctx.excp_mx_linear(x, w, sw, y, c.long(), s),
+                 lambda: ctx.excp_mx_quantize(x, c.long(), s), lambda: ctx.excp_mx_matmul(c.half(), s, w, sw, 256, y),
+                 lambda: ctx.excp_mx_dequantize(c, s.float(), x)):
+        with pytest.raises(TypeError):
+            call()
