@@ -195,7 +195,7 @@ def _pack(w):
     mag = q.abs()
     code = ((mag > 0.25).to(torch.uint8) + (mag > 0.75) + (mag > 1.25) + (mag > 1.75) + (mag > 2.5) + (mag > 3.5)
             + (mag > 5.0) + 8 * torch.signbit(q))
-    code = code.to(torch.uint8).reshape(rows, -1, 2)
+    code = code.reshape(rows, -1, 2)
     return (code[:, :, 0] | (code[:, :, 1] << 4)).contiguous(), (e + 127).to(torch.uint8).contiguous()
 
 
