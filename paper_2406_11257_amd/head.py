@@ -19,24 +19,31 @@ from . import binding as X
 class MxHead:
     """logits = MX(hidden) MX(weight)^T.  weight: a (vocabulary x width) float32, float16 or bfloat16 tensor on the context's
     GPU, read once; with `train` it is kept quantised down its columns too, for the gradient of the hidden states.  Calls may
-    be made from any stream: the context's waits for it, and it for the context's."""
+    be made from any stream: the context's waits for it, and it for the context's.  Results belong to the stream that a call
+    is made from, as torch's own do; `codes` and `codes_t` to the context's, on which all calls read them."""
 
     def __init__(self, ctx: X.Context, weight, train: bool = False):
         self.ctx, (self.vocab, self.width) = ctx, weight.shape
-        with self._on_stream():
+        with self._on_stream(weight):
             self.codes = X.mx_empty(self.vocab, self.width, weight.device)
             self.codes_t = X.mx_empty(self.width, self.vocab, weight.device) if train else (None, None)
             ctx.excp_mx_quantize(weight, *self.codes, *self.codes_t)
 
     @contextlib.contextmanager
-    def _on_stream(self):
-        """The context's stream as the current one, on which what is allocated here is used and given back."""
+    def _on_stream(self, *read):
+        """The context's stream as the current one, for work on the tensors `read` (None: none) and on what the caller's stream
+        has allocated.  That memory goes back to the caller's stream when it is dropped, which waits for the context's, so
+        that no other caller is given it while either may still use it.  (What is allocated on the context's stream inside
+        goes back to that one, and is not for the caller.)"""
         import torch
         own, caller = self.ctx._stream, torch.cuda.current_stream(self.ctx.device)
         if own == caller:
             yield
             return
         own.wait_stream(caller)
+        for t in read:
+            if t is not None and t.is_cuda:
+                t.record_stream(own)                         # whichever stream it was allocated on
         with torch.cuda.stream(own):
             yield
         caller.wait_stream(own)
@@ -49,10 +56,10 @@ class MxHead:
 
         def f32(*shape):
             return torch.empty(*shape, dtype=torch.float32, device=device)
-        with self._on_stream():
-            s = {"logits": f32(tokens, self.vocab), "logprob": f32(tokens), "entropy": f32(tokens), "lse": f32(tokens, 2),
-                 "top_logprob": f32(tokens, ntop) if ntop else None,
-                 "top_ids": torch.empty(tokens, ntop, dtype=torch.int64, device=device) if ntop else None}
+        s = {"logits": f32(tokens, self.vocab), "logprob": f32(tokens), "entropy": f32(tokens), "lse": f32(tokens, 2),
+             "top_logprob": f32(tokens, ntop) if ntop else None,
+             "top_ids": torch.empty(tokens, ntop, dtype=torch.int64, device=device) if ntop else None}
+        with self._on_stream(hidden, targets):
             self.ctx.excp_mx_linear(hidden, *self.codes, s["logits"], *X.mx_empty(tokens, self.width, device))
             self.ctx.excp_token_logprobs(s["logits"], targets, s["logprob"], s["entropy"], s["lse"], s["top_logprob"], s["top_ids"])
         return s
@@ -65,15 +72,15 @@ class MxHead:
             raise ValueError("this head was not made to train")
         tokens, device, ctx = hidden.shape[0], hidden.device, self.ctx
         d = scored["logits"]
-        with self._on_stream():
+        dhidden = torch.empty(tokens, self.width, dtype=torch.float32, device=device)
+        dweight = torch.empty(self.vocab, self.width, dtype=torch.float32, device=device)
+        with self._on_stream(hidden, targets, d, scored["lse"], scored["entropy"], scored["top_ids"], g_logprob, g_entropy, g_top):
             ctx.excp_token_logprobs_backward(d, targets, scored["lse"], scored["entropy"], scored["top_ids"], g_logprob,
                                              g_entropy, g_top, d)
             along, down = X.mx_empty(tokens, self.vocab, device), X.mx_empty(self.vocab, tokens, device)
             hidden_down = X.mx_empty(self.width, tokens, device)
             ctx.excp_mx_quantize(d, *along, *down)
             ctx.excp_mx_quantize(hidden, None, None, *hidden_down)
-            dhidden = torch.empty(tokens, self.width, dtype=torch.float32, device=device)
-            dweight = torch.empty(self.vocab, self.width, dtype=torch.float32, device=device)
             ctx.excp_mx_matmul(*along, *self.codes_t, self.vocab, dhidden)
             ctx.excp_mx_matmul(*down, *hidden_down, tokens, dweight)
         return dhidden, dweight

@@ -99,3 +99,47 @@ def test_a_context_on_another_stream():
 def test_the_command():
     r = head.compare(0, 64)
     assert r["same_first"] > 0.9 and abs(r["logprob"][0] - r["logprob"][1]) < 0.1 and r["compressed"] > 8
+
+
+@pytest.mark.parametrize("what", ["scores", "gradients"])
+def test_two_callers_on_streams_of_their_own(what):
+    """What one caller has dropped and its stream still reads is nobody else's, whoever calls the head meanwhile."""
+    vocab, width, tokens = 5003, 256, 200
+    own, one, two = (torch.cuda.Stream() for _ in range(3))
+    g = torch.Generator(device="cuda")
+    g.manual_seed(11)
+    w = torch.empty(vocab, width, device="cuda").normal_(generator=g)
+    hidden = [torch.empty(tokens, width, device="cuda").normal_(generator=g) for _ in range(2)]
+    targets = torch.randint(0, vocab, (tokens,), device="cuda", generator=g)
+    ones, big = torch.ones(tokens, device="cuda"), torch.empty(4096, 8192, device="cuda")
+    torch.cuda.synchronize()
+
+    def results(hd, h):
+        s = hd.score(h, targets, 3)
+        return [s[k] for k in ("logits", "logprob", "entropy", "lse", "top_logprob", "top_ids")] if what == "scores" else list(hd.gradients(h, targets, s, ones))
+    ctx = X.Context(4096)
+    want = [[t.clone() for t in results(head.MxHead(ctx, w, train=True), h)] for h in hidden]
+    torch.cuda.synchronize()
+    ctx.close()
+    ctx = X.Context(4096, stream=own)
+    hd = head.MxHead(ctx, w, train=True)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(one):
+        first = results(hd, hidden[0])
+        places = {t.data_ptr() for t in first}
+        for _ in range(60):
+            big.normal_()                                    # the reads below are still to come when the others begin
+        kept = [t + 0 for t in first]
+        del first
+    second = []
+    with torch.cuda.stream(two):
+        for _ in range(3):
+            second.append(results(hd, hidden[1]))
+            assert not places & {t.data_ptr() for t in second[-1]}
+    with torch.cuda.stream(own):                             # nor that of another use of the context's stream
+        other = [torch.zeros_like(t) for t in second[0]]
+        assert not places & {t.data_ptr() for t in other}
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(kept, want[0]))
+    assert all(torch.equal(a, b) for s in second for a, b in zip(s, want[1]))
+    ctx.close()
