@@ -44,9 +44,11 @@ class MxHead:
         for t in read:
             if t is not None and t.is_cuda:
                 t.record_stream(own)                         # whichever stream it was allocated on
-        with torch.cuda.stream(own):
-            yield
-        caller.wait_stream(own)
+        try:
+            with torch.cuda.stream(own):
+                yield
+        finally:
+            caller.wait_stream(own)                          # a refusal, too, may leave work that was queued before it
 
     def score(self, hidden, targets, ntop: int = 0) -> dict:
         """hidden: (tokens x width); targets: int64, -1 for a token without one.  Returns the logits (float32), the targets'
