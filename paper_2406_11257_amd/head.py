@@ -68,21 +68,27 @@ class MxHead:
 
     def gradients(self, hidden, targets, scored: dict, g_logprob, g_entropy=None, g_top=None):
         """Of sum(g_logprob logprob) + sum(g_entropy entropy) + sum(g_top top_logprob): (over hidden, over the weight), both
-        float32, from 4-bit products of what is quantised along and down.  The logits of `scored` become their gradient."""
+        float32, from 4-bit products of what is quantised along and down.  The logits of `scored` become their gradient, so
+        that it serves one call; another is refused."""
         import torch
         if self.codes_t[0] is None:
             raise ValueError("this head was not made to train")
-        tokens, device, ctx = hidden.shape[0], hidden.device, self.ctx
         d = scored["logits"]
+        if getattr(d, "holds_gradient", False):
+            raise ValueError("the logits of these scores have become their gradient: score the hidden states again")
+        if hidden.shape != (d.shape[0], self.width):
+            raise ValueError("hidden is not of the shape that was scored")
+        tokens, device, ctx = hidden.shape[0], hidden.device, self.ctx
         dhidden = torch.empty(tokens, self.width, dtype=torch.float32, device=device)
         dweight = torch.empty(self.vocab, self.width, dtype=torch.float32, device=device)
         with self._on_stream(hidden, targets, d, scored["lse"], scored["entropy"], scored["top_ids"], g_logprob, g_entropy, g_top):
-            ctx.excp_token_logprobs_backward(d, targets, scored["lse"], scored["entropy"], scored["top_ids"], g_logprob,
-                                             g_entropy, g_top, d)
             along, down = X.mx_empty(tokens, self.vocab, device), X.mx_empty(self.vocab, tokens, device)
             hidden_down = X.mx_empty(self.width, tokens, device)
-            ctx.excp_mx_quantize(d, *along, *down)
             ctx.excp_mx_quantize(hidden, None, None, *hidden_down)
+            ctx.excp_token_logprobs_backward(d, targets, scored["lse"], scored["entropy"], scored["top_ids"], g_logprob,
+                                             g_entropy, g_top, d)
+            d.holds_gradient = True
+            ctx.excp_mx_quantize(d, *along, *down)
             ctx.excp_mx_matmul(*along, *self.codes_t, self.vocab, dhidden)
             ctx.excp_mx_matmul(*down, *hidden_down, tokens, dweight)
         return dhidden, dweight
