@@ -367,7 +367,7 @@ int excp_mx_matmul(excp_ctx *ctx, const void *a_codes, const void *a_scales, con
 /* y (m x n) = MX(x) W^T for x in 16 or 32 bits: excp_mx_quantize of x and excp_mx_matmul in one call (few
  * rows may go in one kernel, whose fp32 sums are in another order).  x_codes and x_scales (sizes as above for
  * m x k) are room to work in; what they hold afterwards is unspecified.  They may be NULL for up to
- * EXCP_MX_FEW_ROWS rows, which need none. */
+ * EXCP_MX_FEW_ROWS rows, which then need none or work in the context's. */
 #define EXCP_MX_FEW_ROWS 16
 int excp_mx_linear(excp_ctx *ctx, const void *x, int x_type, uint64_t ldx, const void *w_codes,
                    const void *w_scales, uint64_t m, uint64_t n, uint64_t k, void *y, int y_type, uint64_t ldy,

@@ -96,13 +96,16 @@ int excp_mx_linear(excp_ctx *c, const void *x, int x_type, uint64_t ldx, const v
     MxProduct p = {(const unsigned char *)x_codes, (const unsigned char *)x_scales, (const unsigned char *)w_codes,
                    (const unsigned char *)w_scales, {x, ldx, (u32)m, (u32)k, x_type}, y, ldy, (u32)m, (u32)n, groups_of(k), y_type};
     if (m <= EXCP_MX_FEW_ROWS) {
+        // which way they go, and so the order of their sums, is the same whether the caller has given room or not
         const u64 codes = excp_mx_code_bytes(m, k);
         if (codes + excp_mx_scale_bytes(m, k) > sizeof(RowPart) * EXCP_ROW_PARTS || !mx_quantized_first(p, o.cus)) {
             launch_mx_few_rows(p, o.cus, o.stream);
             return launched();
         }
-        p.a_codes = (const unsigned char *)o.parts;          // (the same whether the caller has given room or not)
-        p.a_scales = p.a_codes + codes;
+        if (!x_codes) {
+            p.a_codes = (const unsigned char *)o.parts;
+            p.a_scales = p.a_codes + codes;
+        }
     }
     if (k) launch_mx_quantize({p.x, (unsigned char *)p.a_codes, (unsigned char *)p.a_scales, nullptr, nullptr}, o.cus, o.stream);
     launch_mx_product(p, o.cus, o.stream);

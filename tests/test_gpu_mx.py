@@ -424,3 +424,18 @@ def test_codes_that_are_no_bytes_are_refused(ctx):
                  lambda: ctx.excp_mx_dequantize(c, s.float(), x)):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 16500, 129), (16, 17000, 300), (16, 40, 6657), (16, 20, 63488)])
+def test_few_rows_work_in_the_room_they_are_given(ctx, m, n, k):
+    """Where a few rows take two launches, the codes between them lie in the caller's room, if there is one."""
+    x = draw(m, k, "f32", m + k, 1.0)
+    cb, b = coded(draw(n, k, "f32", n + k + 1, 0.02))
+    room, q = guarded(m, k)
+    y, z = torch.empty(m, n, device="cuda"), torch.empty(m, n, device="cuda")
+    ctx.excp_mx_linear(strided(x, "f32"), *cb, y, *q)
+    ctx.excp_mx_linear(strided(x, "f32"), *cb, z)
+    codes, scales = mx_reference(x)
+    assert np.array_equal(q[0].cpu().numpy(), codes) and np.array_equal(q[1].cpu().numpy(), scales) and unharmed(room, q)
+    assert torch.equal(y, z)
+    assert (np.abs(f64(y) - mx_values(codes, scales, k) @ b.T) <= product_bound(mx_values(codes, scales, k), b, "f32")).all()
