@@ -378,9 +378,7 @@ void launch_tiles(const MxProduct &p, hipStream_t s) {
     k_mx_product<T, TN, TM, WN, WM, KS><<<tiles, L::threads, 0, s>>>(p);
 }
 
-}  // namespace
-
-void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
+void launch_part(const MxProduct &p, u32 cus, hipStream_t s) {
     // The largest tile that gives three workgroups in four compute units and more (a tile's rows are read once for the whole
     // of the other side); where there are no more of the smallest than compute units, four sets of waves a tile.  Measured,
     // m x n x k: 8192 x 8192 x 8192 in tiles of 256: 290 us; 4096 x 2048 x 8192 in 128 tiles of 256: 61 us, of 128: 49;
@@ -400,6 +398,26 @@ void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
         else if (tiles(64u, 64u) > cus) launch_tiles<T, 2, 2, 2, 2, 1>(p, s);
         else launch_tiles<T, 2, 2, 2, 2, 4>(p, s);
     });
+}
+
+}  // namespace
+
+void launch_mx_product(const MxProduct &p, u32 cus, hipStream_t s) {
+    // A launch has fewer than 2^32 threads; a tile has four for a row of its shorter side at most.  (What y can have besides, in
+    // any memory there is, is far less.)
+    constexpr u32 kMost = 1u << 28;
+    for (u32 m = 0; m < p.m; m += kMost)
+        for (u32 n = 0; n < p.n; n += kMost) {
+            MxProduct part = p;
+            part.m = std::min(kMost, p.m - m);
+            part.n = std::min(kMost, p.n - n);
+            part.a_codes += (u64)m * p.groups * 64u;
+            part.a_scales += (u64)m * p.groups * 4u;
+            part.b_codes += (u64)n * p.groups * 64u;
+            part.b_scales += (u64)n * p.groups * 4u;
+            part.y = (unsigned char *)p.y + ((u64)m * p.ld + n) * (p.type == ET_F32 ? 4u : 2u);
+            launch_part(part, cus, s);
+        }
 }
 
 bool mx_quantized_first(const MxProduct &p, u32 cus) {

@@ -439,3 +439,30 @@ def test_few_rows_work_in_the_room_they_are_given(ctx, m, n, k):
     assert np.array_equal(q[0].cpu().numpy(), codes) and np.array_equal(q[1].cpu().numpy(), scales) and unharmed(room, q)
     assert torch.equal(y, z)
     assert (np.abs(f64(y) - mx_values(codes, scales, k) @ b.T) <= product_bound(mx_values(codes, scales, k), b, "f32")).all()
+
+
+def test_more_rows_than_a_launch_has_threads():
+    """2^30 and some rows of W: sixteen million tiles of 256 threads would be more than a launch can have."""
+    n = (1 << 30) + 5
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("needs 80 GB")
+    c = X.Context(4096)
+    codes, scales = (t.zero_() for t in X.mx_empty(n, 1))
+    at = torch.tensor([0, 63, 1 << 28, (1 << 28) + 77, (1 << 29) - 1, 1 << 30, n - 1], device="cuda")
+    codes[at, 0] = 2                                         # 1.0 under 2^0, up to 2^6
+    scales[at, 0] = 127 + torch.arange(7, dtype=torch.uint8, device="cuda")
+    x = torch.ones(1, 1, device="cuda")
+    q = X.mx_empty(1, 1)
+    c.excp_mx_quantize(x, *q)
+    for linear in (False, True):
+        y = torch.full((1, n), 9.0, dtype=torch.float16, device="cuda")
+        if linear:
+            c.excp_mx_linear(x, codes, scales, y)
+        else:
+            c.excp_mx_matmul(*q, codes, scales, 1, y)
+        assert y[0, at].tolist() == [2.0 ** i for i in range(7)]
+        y[0, at] = 0
+        assert not bool(y.any())
+    c.close()
+    del codes, scales, y
+    torch.cuda.empty_cache()
