@@ -290,3 +290,32 @@ def test_refusals(ctx):
                  lambda: ctx.excp_token_logprobs_backward(x, t, v[:, :2].contiguous(), None, None, None, None, None, x.half())):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("parts", [False, True])
+def test_small_probabilities_are_held_to_their_own_size(ctx, parts):
+    """The gradient of improbable tokens, relative to itself: with x - max exact (logits are multiples of 2^-10), p is off by what
+    the sum of exponentials is (2^-22), by what rounds its logarithm (2^-24 of that) and by half a unit of eight operations,
+    however small it is."""
+    rows, vocab = (3, 40001) if parts else (2500, 5003)
+    g = np.random.default_rng(6)
+    x = np.round(-80.0 * g.random((rows, vocab)) * 1024.0) / 1024.0
+    x[:, 7] = 3.0
+    x[1] = np.round(g.standard_normal(vocab) * 2048.0) / 1024.0
+    x[1, 11] = -78.0
+    t = np.full(rows, 7)
+    logits, targets = strided(x, "f32"), torch.from_numpy(t).cuda()
+    o = outputs(rows, 2)
+    ctx.excp_token_logprobs(logits, targets, **o)
+    ones, d = torch.full((rows,), 0.75, device="cuda"), torch.empty_like(logits)
+    z = np.exp(x - x.max(1, keepdims=True))
+    s = z.sum(1, keepdims=True)
+    rel = 2.0 ** -22 + 2.0 ** -24 * (np.abs(np.log(s)) + 8.0)
+    far = np.arange(vocab) != 7
+    ctx.excp_token_logprobs_backward(logits, targets, o["lse"], None, None, ones, None, None, d)
+    assert (np.abs(f64(d) + 0.75 * z / s) <= rel * 0.75 * z / s)[:, far].all()
+    gt = torch.tensor([0.5, 0.25], device="cuda").repeat(rows, 1)
+    ctx.excp_token_logprobs_backward(logits, None, o["lse"], None, o["top_ids"], None, None, gt, d)
+    far = np.ones((rows, vocab), bool)
+    far[np.arange(rows)[:, None], o["top_ids"].cpu().numpy()] = False
+    assert (np.abs(f64(d) + 0.75 * z / s) <= rel * 0.75 * z / s)[far].all()
