@@ -160,13 +160,12 @@ __device__ __forceinline__ void mx_values(u32 codes, float *q) {
 }
 
 // acc += A B^T over 128 elements, for 16 rows of either; lane l holds the 32 codes of row l % 16 from element
-// 32 * (l / 16) on, and their scale in byte BYTE of its scale register.  Result: lane l holds rows
+// 32 * (l / 16) on, and their scale in the lowest byte of its scale register.  Result: lane l holds rows
 // 4 * (l / 16) .. + 3 of A against row l % 16 of B.
-template <int BYTE = 0>
 __device__ __forceinline__ v4f32 mx_mfma(v4i32 a, u32 sa, v4i32 b, u32 sb, v4f32 acc) {
     const v8i32 x = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
     const v8i32 y = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1);
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, BYTE, (int)sa, BYTE, (int)sb);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, 0, (int)sa, 0, (int)sb);
 }
 
 // Memory to LDS without registers: every lane's 16 (4) bytes from its own address, to `to` (the same in every lane)

@@ -15,7 +15,7 @@ constexpr u32 kCandidates = 1024;      // alternatives that are ranked together
 constexpr float kLog2e = 1.44269504088896341f, kLog2eRest = (float)(1.44269504088896341 - kLog2e), kLn2 = 0.69314718055994531f;
 constexpr float kLowest = -3.402823466e38f;
 
-// Sum and largest over a workgroup, in all threads; `room` is used again after the next barrier of the caller only.
+// Sum and largest over a wave, in all lanes.
 __device__ __forceinline__ float wave_sum_f32(float v) {
 #define EXCP_MOVE(CTRL, ROWS) u2f(dpp_u32<CTRL, ROWS>(0u, f2u(v)))
     EXCP_WAVE_SCAN(v, EXCP_FOLD_ADD, EXCP_MOVE);
