@@ -327,7 +327,9 @@ int excp_copy_probe(excp_ctx *ctx, void *dst, const void *src, uint64_t nbytes);
  *
  * What a reconstructed checkpoint is answered and trained with.  The calls below are enqueued on the
  * context's stream and return; they report argument errors at once and have no data-dependent ones, so
- * nothing is collected, and they may be called while a batch is pending.  They allocate nothing.  All
+ * nothing is collected, and they may be called while a batch is pending.  They allocate nothing; some
+ * work in the context's workspace, and a captured call goes on doing so, so that replays of its graph
+ * have to be ordered with the context's other work as calls on its stream are.  All
  * pointers are device memory; a matrix is row-major, its element (i, j) at i * ld + j, ld >= columns;
  * inputs and outputs do not overlap unless a call says so.  Sizes are below 2^31, offsets are 64 bits.
  * Arrays are aligned to their element; code arrays to 16 B and scale arrays to 4 B. */
@@ -375,7 +377,9 @@ int excp_mx_linear(excp_ctx *ctx, const void *x, int x_type, uint64_t ldx, const
 
 /* For every row of logits (rows x vocab): lse = log sum_i exp(x_i), logprob = x[target] - lse, entropy =
  * -sum_i p_i log p_i with p_i = exp(x_i - lse), and the `ntop` largest x_i - lse with their indices, in
- * descending order, equal logits by ascending index.  All statistics in fp32; one read of the logits.
+ * descending order, equal logits by ascending index.  All statistics in fp32.  One read of the logits,
+ * but ntop + 2 of a row in which more than about a thousand are tied for a place among the alternatives
+ * (constant logits; a mask of the type's lowest value that leaves fewer than ntop others).
  *   A logit of -inf is a masked token: p = 0, never an alternative; as a target its logprob is -inf.
  *   A target outside [0, vocab) is none: logprob 0.
  *   Alternatives that do not exist (fewer than ntop unmasked tokens) have index -1 and logprob -inf.
@@ -397,7 +401,8 @@ int excp_token_logprobs(excp_ctx *ctx, const void *logits, int type, uint64_t ro
  *   d_i = g_logprob ([i = target] - p_i) + sum_j g_top_j ([i = top_ids_j] - p_i) - g_entropy p_i (log p_i + entropy)
  * from the lse and entropy (needed with g_entropy) that excp_token_logprobs wrote.  Each g may be NULL (zero); targets are
  * needed with g_logprob, top_ids with g_top.  What has no value in a row -- no target, a masked target,
- * index -1 -- takes no part, and a row with nothing unmasked gets zeros.  dlogits has the logits' type and
+ * index -1 -- takes no part, and a row with nothing unmasked gets zeros.  Of fp32 logits a p_i, however small,
+ * is right to what rounds x_i - largest, the sum and its logarithm to fp32.  dlogits has the logits' type and
  * its own ld, and may be the logits' own array (ldd = ld then; no other overlap). */
 int excp_token_logprobs_backward(excp_ctx *ctx, const void *logits, int type, uint64_t rows, uint64_t vocab,
                                  uint64_t ld, const int64_t *targets, const float *lse, const float *entropy,

@@ -2,8 +2,8 @@
 //
 // With m the largest logit of a row: s = sum exp(x - m), w = sum exp(x - m) (x - m); log p_i = x_i - m - log s, entropy =
 // log s - w / s.  The sums go along with a running m, as each thread sees it, and are brought to a common one in the end.
-// Both passes are bound by memory: the first reads a row once (4096 x 50304 in bf16: 76 us, 5.4 TB/s; 81 with 8 alternatives a
-// row), the second reads and writes it once (169 us, 4.9 TB/s).
+// Both passes are bound by memory: the first reads a row once (4096 x 50304 in bf16: 76 us, 5.4 TB/s, the rate of a large read;
+// 81 with 8 alternatives a row; rows with too many ties among those are read again, see row_part), the second reads and writes it once (169 us, 4.9 TB/s).
 #include "excp_ops_device.h"
 
 #include <type_traits>
@@ -261,7 +261,8 @@ __device__ Sums row_part(const T *x, u32 vocab, u32 begin, u32 end, int ntop, Ro
     if (count <= kCandidates) {
         if (wave == 0) top = first_of(room.candidate, count, (u32)ntop);
     } else {
-        // too many for that (logits that are tied, or laid out so that a few threads hold all large ones): one after another
+        // too many for that (logits that are tied, or laid out so that a few threads hold all large ones): one after another, the
+        // row read for each (4096 x 50304 zeros in bf16 with 8 alternatives: 1.12 ms, 84 us where they differ)
         u64 last = ~0ull;
         for (int j = 0; j < ntop; ++j) {
             u64 next = 0;
