@@ -262,6 +262,8 @@ def _as_bytes(t, stream):
     if t is None or t.dtype is _uint8 or t.dtype not in _wider or not t.is_cuda or not t.is_contiguous():
         return t
     import torch
+    if torch.cuda.current_stream(t.device) == stream:
+        return t.to(_uint8)
     with torch.cuda.stream(stream):
         return t.to(_uint8)
 
